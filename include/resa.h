@@ -17,6 +17,11 @@
  *   resa_dense_rectify    Sec. 2.2  rewrite the last f cache rows, dense
  *                                 causal attention of their queries over the
  *                                 whole cache, refresh the touched summaries
+ *   resa_prompt_attention Alg. 1 prefill of packed prompts of different
+ *                                 lengths: causal attention, grouped heads
+ *   resa_store_rows_q8, resa_load_rows_q8, resa_sparse_decode_q8,
+ *   resa_dense_rectify_q8         the loop's cache calls over an 8-bit cache
+ *                                 with a scale for each block and kv head
  *
  * Conventions shared by every call
  * --------------------------------
@@ -370,6 +375,134 @@ int resa_dense_rectify(const resa_kv_cache_t* c, const void* q_f, const void* k_
                        const int32_t* seq_lens, const int32_t* seq_mask, int32_t max_seq_len,
                        float sm_scale, float* out, float* lse, int32_t refresh_summaries,
                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Causal attention of whole prompts (Alg. 1, prefill), packed one after the
+ * other: sequence s has the n_s = cu_seqlens[s + 1] - cu_seqlens[s] tokens
+ * (any number, zero included) at rows [cu_seqlens[s], cu_seqlens[s + 1]), and
+ * its token i sees its tokens j <= i:
+ *   out[i, h, :] = sum_j softmax_j(q_i,h . k_j * sm_scale) v_j     (bf16)
+ *   lse[i, h]    = log sum_j exp(q_i,h . k_j * sm_scale)  (fp32, may be NULL)
+ * with k, v of kv head h / g. q: bf16 [num_rows, num_q_heads, 128], k, v: bf16
+ * [num_rows, num_kv_heads, 128]; q_stride, k_stride and v_stride are the
+ * elements from a row to the next (multiples of 8, below 2^26, at least a
+ * row's own), so that q, k and v may be parts of one projection's output; a row's heads
+ * are contiguous. out: bf16 [num_rows, num_q_heads, 128], lse: fp32 [num_rows,
+ * num_q_heads], contiguous. cu_seqlens: device int32 [batch + 1],
+ * non-decreasing; its values are cut to [0, num_rows], and rows of no sequence
+ * are neither read nor written. No cache and no workspace is involved.
+ * Precision: scores, softmax and sums in fp32, the weights rounded to bf16 for
+ * the second product, out rounded to bf16; finite for |v| <= 2^96. What a token
+ * does not see never reaches its row, infinities and NaN included.
+ * Errors: RESA_ERR_INVALID_ARG (null or misaligned pointer, a size or stride
+ * out of range, sm_scale not finite), RESA_ERR_UNSUPPORTED (head_dim, group).
+ */
+int resa_prompt_attention(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride,
+                          int64_t v_stride, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                          const int32_t* cu_seqlens, int32_t batch, int32_t num_rows, float sm_scale,
+                          void* out, float* lse, void* stream);
+
+/* Code format of an 8-bit cache. */
+typedef enum resa_q8_format {
+  RESA_Q8_INT8 = 0,  /* two's complement, codes -127 .. 127 (Q = 127) */
+  RESA_Q8_E4M3 = 1   /* OCP 8-bit float, 4 exponent and 3 mantissa bits, no infinities (Q = 448) */
+} resa_q8_format_t;
+
+/*
+ * A KV cache in 8 bits: a value is its code times the scale of its (block, kv
+ * head), one scale for the keys and one for the values. `base` is the cache's
+ * description with k and v pointing at codes (one byte an element, 16-byte
+ * aligned, layouts as in resa_kv_cache_t, paged ones included); its summaries
+ * are those of the bf16 cache. The block selection reads only the summaries, so
+ * resa_select_blocks takes &cache.base; no other call on a resa_kv_cache_t does.
+ */
+typedef struct resa_kv_cache_q8 {
+  resa_kv_cache_t base;
+  float* k_scale;       /* fp32 [batch, num_kv_heads, capacity / block_size]; paged:
+                           [num_pages, num_kv_heads] */
+  float* v_scale;       /* same layout */
+  int32_t format;       /* resa_q8_format_t */
+} resa_kv_cache_q8_t;
+
+/*
+ * Writes the last rows of each sequence into an 8-bit cache and updates the
+ * summaries of the blocks they touch: a prompt, a chunk, a decoded token
+ * (Alg. 1, "Update KV cache / block key cache with t") or rectified rows.
+ * Sequence s has n_s = cu_rows[s + 1] - cu_rows[s] new rows, rows [cu_rows[s],
+ * cu_rows[s + 1]) of k_rows and v_rows (bf16 [num_rows, num_kv_heads, 128],
+ * k_stride / v_stride elements from row to row, multiples of 8, below 2^26),
+ * which become its
+ * positions [L_s - n_s, L_s), L_s = seq_lens[s] already counting them.
+ * For every (block, kv head) touched, keys and values each:
+ *   A     = the largest magnitude of the new rows, at least 2^-100
+ *   scale = A / Q (fp32), where every older row of the block is rewritten or
+ *           there is none; otherwise the larger of A / Q and the block's scale
+ *   code  = value / scale to the nearest code, ties to even; the quotient is
+ *           first rounded to 19 significant bits, so that a tie of the exact
+ *           quotient is one
+ * where the scale of a block that keeps older rows grows, their codes become
+ * code * (old scale / scale), rounded likewise. A row that is not finite gives its
+ * block a scale of NaN, and all of the block's rows then read as NaN.
+ * Summaries (Eq. 3) are of the bf16 keys: of the new rows, and where the block
+ * keeps older rows folded into the block's summary. Rows past L_s keep their
+ * codes. A sequence with n_s = 0, n_s > L_s or L_s > capacity is left as it is,
+ * as are blocks whose table entry lies outside the pool. cu_rows as in
+ * resa_prompt_attention.
+ */
+int resa_store_rows_q8(const resa_kv_cache_q8_t* c, const void* k_rows, const void* v_rows, int64_t k_stride,
+                       int64_t v_stride, const int32_t* cu_rows, int32_t num_rows, const int32_t* seq_lens,
+                       void* stream);
+
+/*
+ * The way back: positions [L_s - n_s, L_s) of each sequence as code * scale,
+ * rounded to bf16, into rows [cu_rows[s], cu_rows[s + 1]) of k_rows and v_rows
+ * (bf16 [num_rows, num_kv_heads, 128], contiguous). Rows of a sequence that the
+ * store above would leave as it is are left as they are.
+ */
+int resa_load_rows_q8(const resa_kv_cache_q8_t* c, const int32_t* cu_rows, int32_t num_rows,
+                      const int32_t* seq_lens, void* k_rows, void* v_rows, void* stream);
+
+/* Workspace bytes resa_sparse_decode_q8 needs (num_splits 0: automatic). */
+size_t resa_decode_q8_workspace_size(int32_t batch, int32_t num_kv_heads, int32_t num_q_heads, int32_t n_cap,
+                                     int32_t block_size, int32_t num_splits);
+
+/*
+ * resa_sparse_decode over an 8-bit cache: the same arguments, results (fp32 out
+ * and lse) and workspace rules, for k = code * k_scale and v = code * v_scale.
+ * Products of codes are exact, weights, sums and scales fp32. Codes of rows
+ * past L_b and of blocks that are not selected are not used, whatever they
+ * hold. A block whose scale is not finite makes the out of the query heads
+ * that attend to it NaN. Value range as in resa_sparse_decode.
+ */
+int resa_sparse_decode_q8(const resa_kv_cache_q8_t* c, const void* q, int32_t num_q_heads,
+                          const int32_t* seq_lens, const int32_t* block_idx, const int32_t* num_sel,
+                          int32_t n_cap, int32_t num_splits, float sm_scale, float* out, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes resa_dense_rectify_q8 needs for any max_seq_len up to the one
+ * given: 0 when one key split covers every such call. */
+size_t resa_rectify_q8_workspace_size(int32_t batch, int32_t num_kv_heads, int32_t num_q_heads,
+                                      int32_t num_rows, int32_t max_seq_len);
+
+/*
+ * Dense rectification (Sec. 2.2) and chunked prefill over an 8-bit cache, for
+ * packed rows: resa_store_rows_q8 of k_rows and v_rows, then the attention of
+ * q_rows (bf16 [num_rows, num_q_heads, 128], q_stride elements from row to
+ * row). Query row r of sequence s sits at position L_s - n_s + r and sees the
+ * cache up to there, its own new rows as they are stored:
+ *   out[cu_rows[s] + r, h, :]  bf16,  lse[cu_rows[s] + r, h]  fp32 or NULL
+ * max_seq_len (host) bounds every seq_lens[s] and lies in [1, capacity]. Rows
+ * of sequences that the store leaves as they are, and of none, keep their out
+ * and lse. A block whose scale is not finite makes the rows that see one of
+ * its keys NaN, and no others. Precision as in resa_prompt_attention. The
+ * workspace holds split partials and needs no initialisation; calls sharing it
+ * must be ordered on one stream.
+ */
+int resa_dense_rectify_q8(const resa_kv_cache_q8_t* c, const void* q_rows, const void* k_rows,
+                          const void* v_rows, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                          int32_t num_q_heads, const int32_t* cu_rows, int32_t num_rows,
+                          const int32_t* seq_lens, int32_t max_seq_len, float sm_scale, void* out, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 /* Zero-fills a workspace with a kernel (safe under stream capture). */
 int resa_workspace_clear(void* workspace, size_t workspace_bytes, void* stream);

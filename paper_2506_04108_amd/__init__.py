@@ -11,20 +11,32 @@ step of the path runs in the library's HIP kernels.
                               min_blocks=128, n_local=1)
     out, lse = sparse_decode(cache, q, seq_lens, idx, nsel)
     dense_rectify(cache, q_f, k_f, v_f, seq_lens, max_seq_len)
+
+Packed prompts and an 8-bit cache (a scale for each block and kv head); rows
+of sequence s are rows [cu[s], cu[s + 1]) of the packed tensors, its last ones:
+
+    out, lse = prompt_attention(q, k, v, cu_seqlens)
+    cache = KVCacheQ8.empty(batch, kv_heads, capacity, block_size, torch.int8)
+    store_rows_q8(cache, k, v, cu_seqlens, seq_lens)        # a prompt, or one token each
+    idx, nsel = select_blocks(cache, q, seq_lens, max_seq_len, ...)
+    out, lse = sparse_decode_q8(cache, q, seq_lens, idx, nsel)
+    out, lse = dense_rectify_q8(cache, q_rows, k_rows, v_rows, cu_rows, seq_lens, max_seq_len)
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import dataclasses
 import math
 
 import torch
 
-from ._lib import KVCacheDesc, ResaError, SelectParams, check, lib
+from ._lib import KVCacheDesc, KVCacheQ8Desc, ResaError, SelectParams, check, lib
 
 __all__ = ["KVCache", "Workspace", "ResaError", "num_selected", "block_summarize", "append_kv",
            "select_blocks", "append_select", "sparse_decode", "decode_step", "dense_rectify",
-           "decode_num_splits", "version"]
+           "decode_num_splits", "version", "KVCacheQ8", "prompt_attention", "store_rows_q8",
+           "load_rows_q8", "sparse_decode_q8", "dense_rectify_q8"]
 
 HEAD_DIM = 128
 
@@ -217,7 +229,8 @@ def select_blocks(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, max_s
     """Pooled-query Quest scores (Eq. 4) and the Eq. 5 top-n per group.
 
     Returns ``(block_idx [B, Hkv, n_cap] int32 ascending, -1 padded,
-    num_sel [B, Hkv] int32)``.
+    num_sel [B, Hkv] int32)``. Reads only the summaries: ``cache`` may be a
+    :class:`KVCacheQ8` too.
     """
     B, Hkv = cache.kmin.shape[0], cache.k.shape[1]
     hq = q.shape[1]
@@ -238,7 +251,7 @@ def select_blocks(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, max_s
     ws = (workspace or Workspace(q.device)).get(ws_bytes)
     ws_ptr, ws_bytes = ws.data_ptr(), ws.numel()
     params = SelectParams(float(sparsity), int(min_blocks), int(n_local))
-    d = cache.desc()
+    d = cache.desc_q8().base if isinstance(cache, KVCacheQ8) else cache.desc()
     check(lib().resa_select_blocks(C.byref(d), q.data_ptr(), hq, seq_lens.data_ptr(), max_seq_len,
                                    C.byref(params), block_idx.data_ptr(), num_sel.data_ptr(), n_cap,
                                    _ptr(scores_out), ws_ptr, ws_bytes, _stream(stream)))
@@ -398,4 +411,269 @@ def dense_rectify(cache: KVCache, q_f: torch.Tensor, k_f: torch.Tensor, v_f: tor
                                    seq_lens.data_ptr(), _ptr(seq_mask), max_seq_len, float(sm_scale),
                                    out.data_ptr(), _ptr(lse), int(bool(refresh)), ws.data_ptr(),
                                    ws.numel(), _stream(stream)))
+    return out, lse
+
+# ------------------------------------------------- packed rows, 8-bit cache
+
+_Q8_FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
+
+
+@dataclasses.dataclass
+class KVCacheQ8:
+    """A layer's KV cache in 8 bits (caller-owned device tensors): a value is
+    its code times the scale of its (block, kv head).
+
+    ``k``, ``v`` hold codes (``torch.int8`` or ``torch.float8_e4m3fn``) in the
+    layouts of :class:`KVCache`, contiguous or paged; ``k_scale``, ``v_scale``
+    are fp32 ``[B, Hkv, capacity / block_size]``, with a block table
+    ``[num_pages, Hkv]``; the summaries are a :class:`KVCache`'s."""
+
+    k: torch.Tensor        # int8 / e4m3 [B, Hkv, capacity, 128] or [num_pages, Hkv, b, 128]
+    v: torch.Tensor
+    k_scale: torch.Tensor  # fp32 [B, Hkv, capacity / block_size] or [num_pages, Hkv]
+    v_scale: torch.Tensor
+    kmin: torch.Tensor     # bf16 [B, Hkv, capacity / block_size, 128]
+    kmax: torch.Tensor
+    block_size: int
+    block_table: torch.Tensor | None = None  # int32 [B, capacity / block_size]
+
+    @classmethod
+    def empty(cls, batch, kv_heads, capacity, block_size, dtype=torch.int8, device="cuda"):
+        mb = capacity // block_size
+        codes = [torch.zeros((batch, kv_heads, capacity, HEAD_DIM), dtype=torch.int8, device=device).view(dtype)
+                 for _ in "kv"]
+        scales = [torch.zeros((batch, kv_heads, mb), dtype=torch.float32, device=device) for _ in "kv"]
+        sums = [torch.zeros((batch, kv_heads, mb, HEAD_DIM), dtype=torch.bfloat16, device=device) for _ in "kv"]
+        return cls(*codes, *scales, *sums, block_size)
+
+    @classmethod
+    def empty_paged(cls, batch, kv_heads, capacity, block_size, num_pages, dtype=torch.int8, device="cuda"):
+        """Zeroed pools of ``num_pages`` pages and a table of -1 (the caller
+        assigns pages)."""
+        mb = capacity // block_size
+        codes = [torch.zeros((num_pages, kv_heads, block_size, HEAD_DIM), dtype=torch.int8,
+                             device=device).view(dtype) for _ in "kv"]
+        scales = [torch.zeros((num_pages, kv_heads), dtype=torch.float32, device=device) for _ in "kv"]
+        sums = [torch.zeros((batch, kv_heads, mb, HEAD_DIM), dtype=torch.bfloat16, device=device) for _ in "kv"]
+        return cls(*codes, *scales, *sums, block_size,
+                   torch.full((batch, mb), -1, dtype=torch.int32, device=device))
+
+    @property
+    def paged(self) -> bool:
+        return self.block_table is not None
+
+    @property
+    def batch(self):
+        return self.kmin.shape[0]
+
+    @property
+    def kv_heads(self):
+        return self.k.shape[1]
+
+    @property
+    def capacity(self):
+        return self.kmin.shape[2] * self.block_size
+
+    def desc(self):
+        raise TypeError("an 8-bit cache: use the calls that end in _q8 (and select_blocks)")
+
+    def desc_q8(self) -> KVCacheQ8Desc:
+        k, b, table = self.k, self.block_size, self.block_table
+        fmt = _Q8_FORMATS.get(k.dtype)
+        if fmt is None:
+            raise TypeError(f"k must be torch.int8 or torch.float8_e4m3fn, got {k.dtype}")
+        B, H, mb = self.kmin.shape[:3]
+        if table is None:
+            shape, pages, tp, scales = (B, H, mb * b, HEAD_DIM), 0, None, (B, H, mb)
+        else:
+            pages = k.shape[0]
+            shape, scales = (pages, H, b, HEAD_DIM), (pages, H)
+            tp = _need(table, "block_table", torch.int32, (B, mb)).data_ptr()
+        _need(k, "k", k.dtype, shape)
+        _need(self.v, "v", k.dtype, shape)
+        _need(self.k_scale, "k_scale", torch.float32, scales)
+        _need(self.v_scale, "v_scale", torch.float32, scales)
+        _need(self.kmin, "kmin", torch.bfloat16, (B, H, mb, HEAD_DIM))
+        _need(self.kmax, "kmax", torch.bfloat16, (B, H, mb, HEAD_DIM))
+        return KVCacheQ8Desc(KVCacheDesc(k.data_ptr(), self.v.data_ptr(), self.kmin.data_ptr(), self.kmax.data_ptr(),
+                                         B, H, HEAD_DIM, mb * b, b, tp, pages),
+                             self.k_scale.data_ptr(), self.v_scale.data_ptr(), fmt)
+
+
+def _packed(t: torch.Tensor, name: str, rows: int, heads: int) -> int:
+    """Checks packed rows ``[rows, heads, 128]`` (bf16, a row contiguous) and
+    returns the elements from one row to the next."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    if t.shape != (rows, heads, HEAD_DIM):
+        raise ValueError(f"{name} must have shape {(rows, heads, HEAD_DIM)}, got {tuple(t.shape)}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient: there is no backward pass")
+    row, head, dim = t.stride()
+    if rows and (dim != 1 or (heads > 1 and head != HEAD_DIM)):
+        raise ValueError(f"{name} must be contiguous within a row")
+    return row if rows > 1 else heads * HEAD_DIM
+
+
+def _same_device(first: torch.Tensor, *others) -> None:
+    """Every tensor of a call is on the current device, whose stream it runs on."""
+    index = first.device.index
+    if index != _current_device():
+        raise ValueError(f"tensors are on device {index}, the current device is {_current_device()}")
+    for t in others:
+        if t is not None and t.device.index != index:
+            raise ValueError(f"tensors are on devices {index} and {t.device.index}")
+
+
+def _allocating(stream):
+    """What a call allocates belongs to the stream that it runs on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
+                     sm_scale: float | None = None, out: torch.Tensor | None = None,
+                     lse: torch.Tensor | None = None, with_lse: bool = True, stream=None):
+    """Causal attention of packed prompts: sequence s has rows ``[cu_seqlens[s],
+    cu_seqlens[s + 1])`` (int32, on the device) of q ``[T, Hq, 128]`` and k, v
+    ``[T, Hkv, 128]`` (bf16; from row to row any stride that is a multiple of
+    8, so that they may be parts of one projection's output). Returns ``(out
+    bf16 [T, Hq, 128], lse fp32 [T, Hq] or None)``; rows of no sequence are
+    not written."""
+    T, hq, hkv = q.shape[0], q.shape[1], k.shape[1]
+    qs, ks, vs = _packed(q, "q", T, hq), _packed(k, "k", T, hkv), _packed(v, "v", T, hkv)
+    B = cu_seqlens.shape[0] - 1
+    _need(cu_seqlens, "cu_seqlens", torch.int32, (B + 1,))
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(HEAD_DIM)
+    with _allocating(stream):
+        if out is None:
+            out = torch.empty((T, hq, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
+        if lse is None and with_lse:
+            lse = torch.empty((T, hq), dtype=torch.float32, device=q.device)
+    _need(out, "out", torch.bfloat16, (T, hq, HEAD_DIM))
+    if lse is not None:
+        _need(lse, "lse", torch.float32, (T, hq))
+    _same_device(q, k, v, cu_seqlens, out, lse)
+    if T:  # an empty tensor has no address
+        check(lib().resa_prompt_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), qs, ks, vs, hq, hkv, HEAD_DIM,
+                                          cu_seqlens.data_ptr(), B, T, float(sm_scale), out.data_ptr(), _ptr(lse),
+                                          _stream(stream)))
+    return out, lse
+
+
+def store_rows_q8(cache: KVCacheQ8, k_rows: torch.Tensor, v_rows: torch.Tensor, cu_rows: torch.Tensor,
+                  seq_lens: torch.Tensor, stream=None) -> None:
+    """The last rows of each sequence into an 8-bit cache (a prompt, a chunk,
+    one decoded token), with the summaries of the blocks they touch. Rows
+    ``[cu_rows[s], cu_rows[s + 1])`` of k_rows, v_rows ``[T, Hkv, 128]`` (bf16)
+    become the last positions of sequence s, whose ``seq_lens`` already counts
+    them."""
+    T = k_rows.shape[0]
+    ks, vs = _packed(k_rows, "k_rows", T, cache.kv_heads), _packed(v_rows, "v_rows", T, cache.kv_heads)
+    _need(cu_rows, "cu_rows", torch.int32, (cache.batch + 1,))
+    _need(seq_lens, "seq_lens", torch.int32, (cache.batch,))
+    d = cache.desc_q8()
+    _same_device(cache.k, k_rows, v_rows, cu_rows, seq_lens)
+    if T:
+        check(lib().resa_store_rows_q8(C.byref(d), k_rows.data_ptr(), v_rows.data_ptr(), ks, vs, cu_rows.data_ptr(),
+                                       T, seq_lens.data_ptr(), _stream(stream)))
+
+
+def load_rows_q8(cache: KVCacheQ8, cu_rows: torch.Tensor, seq_lens: torch.Tensor, num_rows: int | None = None,
+                 out: tuple | None = None, stream=None):
+    """The last rows of each sequence as bf16, ``(k_rows, v_rows)`` of ``[T,
+    Hkv, 128]``: ``out``, or new tensors of ``num_rows`` rows."""
+    if out is None:
+        if num_rows is None:
+            raise ValueError("either num_rows or out must be given")
+        with _allocating(stream):
+            out = tuple(torch.empty((num_rows, cache.kv_heads, HEAD_DIM), dtype=torch.bfloat16,
+                                    device=cache.k.device) for _ in "kv")
+    k_rows, v_rows = out
+    T = k_rows.shape[0]
+    _need(k_rows, "k_rows", torch.bfloat16, (T, cache.kv_heads, HEAD_DIM))
+    _need(v_rows, "v_rows", torch.bfloat16, (T, cache.kv_heads, HEAD_DIM))
+    _need(cu_rows, "cu_rows", torch.int32, (cache.batch + 1,))
+    _need(seq_lens, "seq_lens", torch.int32, (cache.batch,))
+    d = cache.desc_q8()
+    _same_device(cache.k, k_rows, v_rows, cu_rows, seq_lens)
+    if T:
+        check(lib().resa_load_rows_q8(C.byref(d), cu_rows.data_ptr(), T, seq_lens.data_ptr(), k_rows.data_ptr(),
+                                      v_rows.data_ptr(), _stream(stream)))
+    return k_rows, v_rows
+
+
+def sparse_decode_q8(cache: KVCacheQ8, q: torch.Tensor, seq_lens: torch.Tensor, block_idx: torch.Tensor,
+                     num_sel: torch.Tensor, num_splits: int = 0, sm_scale: float | None = None,
+                     out: torch.Tensor | None = None, lse: torch.Tensor | None = None, with_lse: bool = True,
+                     workspace: Workspace | None = None, stream=None):
+    """:func:`sparse_decode` over an 8-bit cache. Returns ``(out fp32 [B, Hq,
+    128], lse fp32 [B, Hq] or None)``."""
+    B, Hkv = cache.kmin.shape[0], cache.k.shape[1]
+    hq = q.shape[1]
+    _need(q, "q", torch.bfloat16, (B, hq, HEAD_DIM))
+    _need(seq_lens, "seq_lens", torch.int32, (B,))
+    n_cap = block_idx.shape[-1]
+    _need(block_idx, "block_idx", torch.int32, (B, Hkv, n_cap))
+    _need(num_sel, "num_sel", torch.int32, (B, Hkv))
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(HEAD_DIM)
+    ws_bytes = lib().resa_decode_q8_workspace_size(B, Hkv, hq, n_cap, cache.block_size, num_splits)
+    with _allocating(stream):
+        if out is None:
+            out = torch.empty((B, hq, HEAD_DIM), dtype=torch.float32, device=q.device)
+        if lse is None and with_lse:
+            lse = torch.empty((B, hq), dtype=torch.float32, device=q.device)
+        ws = (workspace or Workspace(q.device)).get(ws_bytes)
+    _need(out, "out", torch.float32, (B, hq, HEAD_DIM))
+    if lse is not None:
+        _need(lse, "lse", torch.float32, (B, hq))
+    d = cache.desc_q8()
+    _same_device(cache.k, q, seq_lens, block_idx, num_sel, out, lse, ws)
+    check(lib().resa_sparse_decode_q8(C.byref(d), q.data_ptr(), hq, seq_lens.data_ptr(), block_idx.data_ptr(),
+                                      num_sel.data_ptr(), n_cap, num_splits, float(sm_scale), out.data_ptr(),
+                                      _ptr(lse), ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out, lse
+
+
+def dense_rectify_q8(cache: KVCacheQ8, q_rows: torch.Tensor, k_rows: torch.Tensor, v_rows: torch.Tensor,
+                     cu_rows: torch.Tensor, seq_lens: torch.Tensor, max_seq_len: int,
+                     sm_scale: float | None = None, out: torch.Tensor | None = None,
+                     lse: torch.Tensor | None = None, with_lse: bool = True,
+                     workspace: Workspace | None = None, stream=None):
+    """Rectification (Sec. 2.2) or a prompt chunk over an 8-bit cache:
+    :func:`store_rows_q8` of the packed k_rows, v_rows, then dense causal
+    attention of q_rows ``[T, Hq, 128]`` (bf16) over the whole cache.
+    ``max_seq_len`` bounds seq_lens. Returns ``(out bf16 [T, Hq, 128], lse fp32
+    [T, Hq] or None)``; rows of sequences without rows in the call are not
+    written."""
+    B, Hkv = cache.kmin.shape[0], cache.k.shape[1]
+    T, hq = q_rows.shape[0], q_rows.shape[1]
+    qs = _packed(q_rows, "q_rows", T, hq)
+    ks, vs = _packed(k_rows, "k_rows", T, Hkv), _packed(v_rows, "v_rows", T, Hkv)
+    _need(cu_rows, "cu_rows", torch.int32, (B + 1,))
+    _need(seq_lens, "seq_lens", torch.int32, (B,))
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(HEAD_DIM)
+    ws_bytes = lib().resa_rectify_q8_workspace_size(B, Hkv, hq, T, max_seq_len)
+    with _allocating(stream):
+        if out is None:
+            out = torch.empty((T, hq, HEAD_DIM), dtype=torch.bfloat16, device=q_rows.device)
+        if lse is None and with_lse:
+            lse = torch.empty((T, hq), dtype=torch.float32, device=q_rows.device)
+        ws = (workspace or Workspace(q_rows.device)).get(ws_bytes)
+    _need(out, "out", torch.bfloat16, (T, hq, HEAD_DIM))
+    if lse is not None:
+        _need(lse, "lse", torch.float32, (T, hq))
+    d = cache.desc_q8()
+    _same_device(cache.k, q_rows, k_rows, v_rows, cu_rows, seq_lens, out, lse, ws)
+    if T:
+        check(lib().resa_dense_rectify_q8(C.byref(d), q_rows.data_ptr(), k_rows.data_ptr(), v_rows.data_ptr(), qs, ks,
+                                          vs, hq, cu_rows.data_ptr(), T, seq_lens.data_ptr(), max_seq_len,
+                                          float(sm_scale), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(),
+                                          _stream(stream)))
     return out, lse

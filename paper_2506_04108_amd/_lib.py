@@ -29,6 +29,10 @@ class KVCacheDesc(C.Structure):
                 ("block_table", C.c_void_p), ("num_pages", C.c_int32)]
 
 
+class KVCacheQ8Desc(C.Structure):
+    _fields_ = [("base", KVCacheDesc), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("format", C.c_int32)]
+
+
 class SelectParams(C.Structure):
     _fields_ = [("sparsity", C.c_double), ("min_blocks", C.c_int32), ("n_local", C.c_int32)]
 
@@ -38,7 +42,9 @@ _I = C.c_int32
 _Z = C.c_size_t
 _F = C.c_float
 _D = C.c_double
+_L = C.c_int64
 _CACHE = C.POINTER(KVCacheDesc)
+_CACHE_Q8 = C.POINTER(KVCacheQ8Desc)
 
 # name -> (restype, argtypes); mirrors include/resa.h.
 SIGNATURES = {
@@ -65,6 +71,14 @@ SIGNATURES = {
     "resa_rectify_workspace_size": (_Z, [_I, _I, _I, _I, _I]),
     "resa_dense_rectify": (C.c_int, [_CACHE, _P, _P, _P, _I, _I, _P, _P, _I, _F, _P, _P, _I, _P,
                                      _Z, _P]),
+    "resa_prompt_attention": (C.c_int, [_P, _P, _P, _L, _L, _L, _I, _I, _I, _P, _I, _I, _F, _P, _P, _P]),
+    "resa_store_rows_q8": (C.c_int, [_CACHE_Q8, _P, _P, _L, _L, _P, _I, _P, _P]),
+    "resa_load_rows_q8": (C.c_int, [_CACHE_Q8, _P, _I, _P, _P, _P, _P]),
+    "resa_decode_q8_workspace_size": (_Z, [_I, _I, _I, _I, _I, _I]),
+    "resa_sparse_decode_q8": (C.c_int, [_CACHE_Q8, _P, _I, _P, _P, _P, _I, _I, _F, _P, _P, _P, _Z, _P]),
+    "resa_rectify_q8_workspace_size": (_Z, [_I, _I, _I, _I, _I]),
+    "resa_dense_rectify_q8": (C.c_int, [_CACHE_Q8, _P, _P, _P, _L, _L, _L, _I, _P, _I, _P, _I, _F, _P, _P,
+                                        _P, _Z, _P]),
     "resa_workspace_clear": (C.c_int, [_P, _Z, _P]),
     "resa_stream_read": (C.c_int, [_P, _Z, _P, C.c_uint32, _I, _P]),
 }

@@ -441,14 +441,10 @@ int decode_check(const resa_kv_cache_t* c, const void* q, int32_t num_q_heads,
   return RESA_OK;
 }
 
-// Enqueues the decode on checked arguments with the workspace at `ws`.
-// `clear_counters` first zero-fills the merge counters with a kernel (the
-// allocation-free variant, whose scratch every call on the device shares).
-int decode_launch(const resa_kv_cache_t* c, const void* q, int32_t num_q_heads,
-                  const int32_t* seq_lens, const int32_t* block_idx, const int32_t* num_sel,
-                  int32_t n_cap, int32_t group, int32_t splits, float sm_scale, float* out,
-                  float* lse, char* ws, const DecodeLayout& lay, bool clear_counters, void* stream,
-                  const char* what) {
+resa::DecodeArgs decode_args(const resa_kv_cache_t* c, const void* q, int32_t num_q_heads, const int32_t* seq_lens,
+                             const int32_t* block_idx, const int32_t* num_sel, int32_t n_cap, int32_t group,
+                             int32_t splits, float sm_scale, float* out, float* lse, char* ws,
+                             const DecodeLayout& lay) {
   resa::DecodeArgs a;
   a.c = cache_args(c);
   a.q = static_cast<const uint16_t*>(q);
@@ -467,6 +463,19 @@ int decode_launch(const resa_kv_cache_t* c, const void* q, int32_t num_q_heads,
   a.flags = reinterpret_cast<uint64_t*>(ws + lay.flags);
   a.part_lse = reinterpret_cast<float*>(ws + lay.lse);
   a.part_o = reinterpret_cast<float*>(ws + lay.o);
+  return a;
+}
+
+// Enqueues the decode on checked arguments with the workspace at `ws`.
+// `clear_counters` first zero-fills the merge counters with a kernel (the
+// allocation-free variant, whose scratch every call on the device shares).
+int decode_launch(const resa_kv_cache_t* c, const void* q, int32_t num_q_heads,
+                  const int32_t* seq_lens, const int32_t* block_idx, const int32_t* num_sel,
+                  int32_t n_cap, int32_t group, int32_t splits, float sm_scale, float* out,
+                  float* lse, char* ws, const DecodeLayout& lay, bool clear_counters, void* stream,
+                  const char* what) {
+  const resa::DecodeArgs a = decode_args(c, q, num_q_heads, seq_lens, block_idx, num_sel, n_cap, group, splits,
+                                         sm_scale, out, lse, ws, lay);
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (clear_counters) {
     hipError_t e = resa::launch_clear(ws + lay.counters, lay.lse - lay.counters, st);
@@ -697,6 +706,261 @@ int resa_dense_rectify(const resa_kv_cache_t* c, const void* q_f, const void* k_
   a.seq_mask = seq_mask;
   hipError_t e = resa::launch_rectify(a, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "resa_dense_rectify launch");
+  return ok();
+}
+
+namespace {
+
+// Strides count elements and a tile's rows are addressed with 32 bits.
+constexpr int64_t kMaxStride = int64_t(1) << 26;
+
+int check_stride(const char* name, int64_t stride, int32_t heads) {
+  if (stride < (int64_t)heads * RESA_HEAD_DIM || stride % 8 != 0 || stride >= kMaxStride)
+    return fail(RESA_ERR_INVALID_ARG, "%s %lld is not a multiple of 8 in [%d * %d, 2^26)", name, (long long)stride,
+                heads, RESA_HEAD_DIM);
+  return RESA_OK;
+}
+
+int check_cache_q8(const resa_kv_cache_q8_t* c) {
+  if (c == nullptr) return fail(RESA_ERR_INVALID_ARG, "cache descriptor is NULL");
+  if (int e = check_cache(&c->base)) return e;
+  RESA_CHECK_PTR(c->k_scale, 4);
+  RESA_CHECK_PTR(c->v_scale, 4);
+  if (c->format != RESA_Q8_INT8 && c->format != RESA_Q8_E4M3)
+    return fail(RESA_ERR_UNSUPPORTED, "8-bit format %d unsupported", c->format);
+  return RESA_OK;
+}
+
+int rows_q8_args(const resa_kv_cache_q8_t* c, const int32_t* cu_rows, int32_t num_rows, const int32_t* seq_lens,
+                 resa::RowsQ8Args* a) {
+  if (int e = check_cache_q8(c)) return e;
+  RESA_CHECK_PTR(cu_rows, 4);
+  RESA_CHECK_PTR(seq_lens, 4);
+  if (num_rows < 0) return fail(RESA_ERR_INVALID_ARG, "num_rows %d < 0", num_rows);
+  if (((int64_t)num_rows / c->base.block_size + 2 * (int64_t)c->base.batch) * c->base.num_kv_heads > INT32_MAX)
+    return fail(RESA_ERR_UNSUPPORTED, "%d rows of %d heads are more than one launch takes", num_rows,
+                c->base.num_kv_heads);
+  *a = {};
+  a->c = cache_args(&c->base);
+  a->k_scale = c->k_scale;
+  a->v_scale = c->v_scale;
+  a->format = c->format;
+  a->cu = cu_rows;
+  a->rows = num_rows;
+  a->seq_lens = seq_lens;
+  return RESA_OK;
+}
+
+// Argument checks of resa_store_rows_q8 (also those of resa_dense_rectify_q8).
+int store_rows_q8_args(const resa_kv_cache_q8_t* c, const void* k_rows, const void* v_rows, int64_t k_stride,
+                       int64_t v_stride, const int32_t* cu_rows, int32_t num_rows, const int32_t* seq_lens,
+                       resa::RowsQ8Args* a) {
+  if (int e = rows_q8_args(c, cu_rows, num_rows, seq_lens, a)) return e;
+  RESA_CHECK_PTR(k_rows, 16);
+  RESA_CHECK_PTR(v_rows, 16);
+  if (int e = check_stride("k_stride", k_stride, c->base.num_kv_heads)) return e;
+  if (int e = check_stride("v_stride", v_stride, c->base.num_kv_heads)) return e;
+  a->k_rows = static_cast<const uint16_t*>(k_rows);
+  a->v_rows = static_cast<const uint16_t*>(v_rows);
+  a->k_stride = k_stride;
+  a->v_stride = v_stride;
+  return RESA_OK;
+}
+
+// Upper bound of the workgroups of an attention over packed rows.
+bool rows_grid_fits(int32_t batch, int32_t rows, int32_t group, int32_t kv_heads, int32_t splits) {
+  return ((int64_t)rows * group / 128 + batch) * splits <= INT32_MAX / kv_heads;
+}
+
+struct RowsLayout {
+  int32_t chunk, splits;
+  size_t lse, o, total;
+};
+
+RowsLayout rows_layout(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
+  RowsLayout l;
+  l.chunk = resa::rows_chunk(batch, kv_heads, group, rows, max_seq_len);
+  l.splits = (max_seq_len + l.chunk - 1) / l.chunk;
+  if (l.splits < 1) l.splits = 1;
+  const size_t outs = (size_t)rows * kv_heads * group;
+  l.lse = 0;
+  l.o = round256(outs * l.splits * 4);
+  l.total = l.splits == 1 ? 0 : l.o + outs * l.splits * RESA_HEAD_DIM * 4;
+  return l;
+}
+
+}  // namespace
+
+int resa_prompt_attention(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride,
+                          int64_t v_stride, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                          const int32_t* cu_seqlens, int32_t batch, int32_t num_rows, float sm_scale, void* out,
+                          float* lse, void* stream) {
+  RESA_CHECK_PTR(q, 16);
+  RESA_CHECK_PTR(k, 16);
+  RESA_CHECK_PTR(v, 16);
+  RESA_CHECK_PTR(cu_seqlens, 4);
+  RESA_CHECK_PTR(out, 16);
+  if (lse != nullptr && !aligned(lse, 4)) return fail(RESA_ERR_INVALID_ARG, "lse is not 4-byte aligned");
+  if (head_dim != RESA_HEAD_DIM) return fail(RESA_ERR_UNSUPPORTED, "head_dim %d unsupported (only 128)", head_dim);
+  if (batch < 1 || num_kv_heads < 1 || num_rows < 0)
+    return fail(RESA_ERR_INVALID_ARG, "batch (%d) and num_kv_heads (%d) must be >= 1, num_rows (%d) >= 0", batch,
+                num_kv_heads, num_rows);
+  if ((int64_t)batch * num_kv_heads > 65535)
+    return fail(RESA_ERR_UNSUPPORTED, "batch * num_kv_heads = %lld exceeds 65535", (long long)batch * num_kv_heads);
+  if (num_q_heads < 1 || num_q_heads % num_kv_heads != 0)
+    return fail(RESA_ERR_INVALID_ARG, "num_q_heads %d is not a positive multiple of num_kv_heads %d", num_q_heads,
+                num_kv_heads);
+  const int32_t group = num_q_heads / num_kv_heads;
+  if (group > RESA_MAX_GROUP) return fail(RESA_ERR_UNSUPPORTED, "group size %d exceeds %d", group, RESA_MAX_GROUP);
+  if (int e = check_stride("q_stride", q_stride, num_q_heads)) return e;
+  if (int e = check_stride("k_stride", k_stride, num_kv_heads)) return e;
+  if (int e = check_stride("v_stride", v_stride, num_kv_heads)) return e;
+  if (!std::isfinite(sm_scale)) return fail(RESA_ERR_INVALID_ARG, "sm_scale is not finite");
+  if (num_rows > INT32_MAX / RESA_MAX_GROUP || !rows_grid_fits(batch, num_rows, group, num_kv_heads, 1))
+    return fail(RESA_ERR_UNSUPPORTED, "%d rows of %d heads are more than one launch takes", num_rows, num_q_heads);
+  if (num_rows == 0) return ok();
+  resa::RowsArgs a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.cu = cu_seqlens;
+  a.batch = batch;
+  a.rows = num_rows;
+  a.q_heads = num_q_heads;
+  a.kv_heads = num_kv_heads;
+  a.group = group;
+  a.chunk = INT32_MAX;
+  a.num_splits = 1;
+  a.scale_log2 = sm_scale * 1.4426950408889634f;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  hipError_t e = resa::launch_prompt(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "resa_prompt_attention launch");
+  return ok();
+}
+
+int resa_store_rows_q8(const resa_kv_cache_q8_t* c, const void* k_rows, const void* v_rows, int64_t k_stride,
+                       int64_t v_stride, const int32_t* cu_rows, int32_t num_rows, const int32_t* seq_lens,
+                       void* stream) {
+  resa::RowsQ8Args a;
+  if (int e = store_rows_q8_args(c, k_rows, v_rows, k_stride, v_stride, cu_rows, num_rows, seq_lens, &a)) return e;
+  if (num_rows == 0) return ok();
+  hipError_t e = resa::launch_store_rows_q8(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "resa_store_rows_q8 launch");
+  return ok();
+}
+
+int resa_load_rows_q8(const resa_kv_cache_q8_t* c, const int32_t* cu_rows, int32_t num_rows, const int32_t* seq_lens,
+                      void* k_rows, void* v_rows, void* stream) {
+  resa::RowsQ8Args a;
+  if (int e = rows_q8_args(c, cu_rows, num_rows, seq_lens, &a)) return e;
+  RESA_CHECK_PTR(k_rows, 16);
+  RESA_CHECK_PTR(v_rows, 16);
+  if (num_rows == 0) return ok();
+  a.k_out = static_cast<uint16_t*>(k_rows);
+  a.v_out = static_cast<uint16_t*>(v_rows);
+  hipError_t e = resa::launch_load_rows_q8(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "resa_load_rows_q8 launch");
+  return ok();
+}
+
+size_t resa_decode_q8_workspace_size(int32_t batch, int32_t num_kv_heads, int32_t num_q_heads, int32_t n_cap,
+                                     int32_t block_size, int32_t num_splits) {
+  if (batch < 1 || num_kv_heads < 1 || num_q_heads < num_kv_heads || n_cap < 0 || block_size < 16 || num_splits < 0)
+    return 0;
+  const int32_t s = num_splits > 0 ? num_splits
+                                   : resa::decode_q8_auto_splits(batch, num_kv_heads, n_cap, block_size);
+  return decode_layout(batch, num_kv_heads, num_q_heads / num_kv_heads, s).total;
+}
+
+int resa_sparse_decode_q8(const resa_kv_cache_q8_t* c, const void* q, int32_t num_q_heads, const int32_t* seq_lens,
+                          const int32_t* block_idx, const int32_t* num_sel, int32_t n_cap, int32_t num_splits,
+                          float sm_scale, float* out, float* lse, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  if (int e = check_cache_q8(c)) return e;
+  int32_t group = 0, splits = 0;
+  DecodeLayout lay;
+  const int32_t want = num_splits != 0 || n_cap < 0 ? num_splits
+                       : resa::decode_q8_auto_splits(c->base.batch, c->base.num_kv_heads, n_cap, c->base.block_size);
+  if (int e = decode_check(&c->base, q, num_q_heads, seq_lens, block_idx, num_sel, n_cap, want, sm_scale, out, lse,
+                           &group, &splits, &lay))
+    return e;
+  if (workspace == nullptr || workspace_bytes < lay.total)
+    return fail(RESA_ERR_WORKSPACE, "decode workspace needs %zu bytes, got %zu", lay.total,
+                workspace == nullptr ? (size_t)0 : workspace_bytes);
+  if (!aligned(workspace, 16)) return fail(RESA_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+  const resa::DecodeArgs a = decode_args(&c->base, q, num_q_heads, seq_lens, block_idx, num_sel, n_cap, group, splits,
+                                         sm_scale, out, lse, static_cast<char*>(workspace), lay);
+  hipError_t e = resa::launch_decode_q8(a, c->k_scale, c->v_scale, c->format, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "resa_sparse_decode_q8 launch");
+  return ok();
+}
+
+size_t resa_rectify_q8_workspace_size(int32_t batch, int32_t num_kv_heads, int32_t num_q_heads, int32_t num_rows,
+                                      int32_t max_seq_len) {
+  if (batch < 1 || num_kv_heads < 1 || num_q_heads < num_kv_heads || num_rows < 1 || max_seq_len < 1) return 0;
+  const int32_t group = num_q_heads / num_kv_heads;
+  const size_t most = (size_t)resa::rows_max_splits(batch, num_kv_heads, group, num_rows, max_seq_len);
+  if (most == 1) return 0;
+  const size_t outs = (size_t)num_rows * num_kv_heads * group;
+  return round256(outs * most * 4) + outs * most * RESA_HEAD_DIM * 4;
+}
+
+int resa_dense_rectify_q8(const resa_kv_cache_q8_t* c, const void* q_rows, const void* k_rows, const void* v_rows,
+                          int64_t q_stride, int64_t k_stride, int64_t v_stride, int32_t num_q_heads,
+                          const int32_t* cu_rows, int32_t num_rows, const int32_t* seq_lens, int32_t max_seq_len,
+                          float sm_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  resa::RowsQ8Args store;
+  if (int e = store_rows_q8_args(c, k_rows, v_rows, k_stride, v_stride, cu_rows, num_rows, seq_lens, &store)) return e;
+  const resa_kv_cache_t* b = &c->base;
+  int32_t group = 0;
+  if (int e = check_heads(b, num_q_heads, &group)) return e;
+  RESA_CHECK_PTR(q_rows, 16);
+  if (int e = check_stride("q_stride", q_stride, num_q_heads)) return e;
+  RESA_CHECK_PTR(out, 16);
+  if (lse != nullptr && !aligned(lse, 4)) return fail(RESA_ERR_INVALID_ARG, "lse is not 4-byte aligned");
+  if (max_seq_len < 1 || max_seq_len > b->capacity)
+    return fail(RESA_ERR_INVALID_ARG, "max_seq_len %d outside [1, capacity %d]", max_seq_len, b->capacity);
+  if (!std::isfinite(sm_scale)) return fail(RESA_ERR_INVALID_ARG, "sm_scale is not finite");
+  if (num_rows == 0) return ok();
+  const RowsLayout lay = rows_layout(b->batch, b->num_kv_heads, group, num_rows, max_seq_len);
+  if (num_rows > INT32_MAX / RESA_MAX_GROUP || !rows_grid_fits(b->batch, num_rows, group, b->num_kv_heads, lay.splits))
+    return fail(RESA_ERR_UNSUPPORTED, "%d rows of %d heads are more than one launch takes", num_rows, num_q_heads);
+  if (lay.total > 0 && (workspace == nullptr || workspace_bytes < lay.total))
+    return fail(RESA_ERR_WORKSPACE, "rectify workspace needs %zu bytes, got %zu", lay.total,
+                workspace == nullptr ? (size_t)0 : workspace_bytes);
+  if (workspace != nullptr && !aligned(workspace, 16))
+    return fail(RESA_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+  char* ws = static_cast<char*>(workspace);
+  resa::RowsArgs a = {};
+  a.c = store.c;
+  a.k_scale = c->k_scale;
+  a.v_scale = c->v_scale;
+  a.seq_lens = seq_lens;
+  a.q = static_cast<const uint16_t*>(q_rows);
+  a.q_stride = q_stride;
+  a.cu = cu_rows;
+  a.batch = b->batch;
+  a.rows = num_rows;
+  a.q_heads = num_q_heads;
+  a.kv_heads = b->num_kv_heads;
+  a.group = group;
+  a.chunk = lay.chunk;
+  a.num_splits = lay.splits;
+  a.scale_log2 = sm_scale * 1.4426950408889634f;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  if (lay.splits > 1) {
+    a.part_lse = reinterpret_cast<float*>(ws + lay.lse);
+    a.part_o = reinterpret_cast<float*>(ws + lay.o);
+  }
+  hipError_t e = resa::launch_store_rows_q8(store, static_cast<hipStream_t>(stream));
+  if (e == hipSuccess) e = resa::launch_rows_q8(a, c->format, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "resa_dense_rectify_q8 launch");
   return ok();
 }
 

@@ -403,6 +403,103 @@ constexpr uint32_t kFlagSpins = 1u << 22;
 // query head each (merge_head), instead of done by the last one alone.
 constexpr int kSpreadSplits = 16;
 
+// The end of a split, whose normalised partial and lse (log2 domain) the
+// threads hold: item it = tid + k NT of two dims each is head it / 64, dims
+// 2 (it % 64) .. . A single split writes the output; otherwise the partial is
+// published and the last split(s) of the group merge all of them. `ticket` is
+// the split's place among the group's splits to finish (in thread 0), `epoch`
+// the group's count of merged calls.
+template <int G, int NW, class Lds>
+__device__ __forceinline__ void finish_split(const DecodeArgs& a, size_t grp, int split, size_t ob, uint32_t ticket,
+                                             uint32_t epoch, const f2_t (&val)[(G * 64 + 64 * NW - 1) / (64 * NW)],
+                                             const float (&lg)[(G * 64 + 64 * NW - 1) / (64 * NW)], Lds& lds) {
+  constexpr int NT2 = 64 * NW;
+  constexpr int kItems = (G * 64 + NT2 - 1) / NT2;
+  const int tid = threadIdx.x;
+  const int S = a.num_splits;
+  const bool single = S == 1;
+  const float ninf = -__builtin_inff();
+  if (single) {
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int it = tid + k * NT2;
+      if (it < G * 64) {
+        *reinterpret_cast<f2_t*>(a.out + ob * kHeadDim + 2 * it) = val[k];
+        if (it % 64 == 0 && a.lse) a.lse[ob + it / 64] = lg[k] == ninf ? ninf : lg[k] * kLn2;
+      }
+    }
+    return;
+  }
+  if (tid == 0) lds.ticket = ticket;
+  lds_sync();
+  // The call count read at the start is first used here: it stays in a
+  // vector register until now, so no earlier instruction waits for it.
+  __asm__ volatile("" : "+v"(epoch));
+  // Merging splits: the one holding the last ticket, or with many splits
+  // those holding the last G tickets, one query head each. A ready flag
+  // carries this call's tag (the group's merged-call count + 1, and S), so
+  // flags left by earlier calls never match and no flag is ever reset; the
+  // split holding the last ticket returns the ticket counter to zero and
+  // advances the count once every ticket is taken.
+  const uint32_t tk = lds.ticket;
+  const bool spread = G >= 2 && S >= kSpreadSplits && S >= G;
+  const uint32_t first = spread ? (uint32_t)(S - G) : (uint32_t)(S - 1);
+  const uint64_t tag = ((uint64_t)(epoch + 1u) << 32) | (uint32_t)S;
+  if (spread || tk < first) {
+    // Publish: agent-scope stores write through to the level every L2 slice
+    // reads (sc1), every thread waits for their acknowledgement, then one
+    // thread raises the split's ready flag.
+    float* po = a.part_o + (grp * S + split) * (size_t)(G * kHeadDim);
+    float* pl = a.part_lse + (grp * S + split) * (size_t)G;
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int it = tid + k * NT2;
+      if (it < G * 64) {
+        __hip_atomic_store(po + 2 * it, val[k].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(po + 2 * it + 1, val[k].y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (it % 64 == 0) __hip_atomic_store(pl + it / 64, lg[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    }
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) __hip_atomic_store(a.flags + grp * S + split, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tk < first) return;
+  }
+
+  // Alg. 2, "Combine", in a merging split: its own partial stays in LDS;
+  // every other split has taken its ticket and is publishing (or has), so
+  // thread t < S waits for split t's flag (agent-scope loads), then the
+  // partials are read with agent-scope loads and merged.
+#pragma unroll
+  for (int k = 0; k < kItems; ++k) {
+    const int it = tid + k * NT2;
+    if (it < G * 64) {
+      *reinterpret_cast<f2_t*>(&lds.own_o[2 * it]) = val[k];
+      if (it % 64 == 0) lds.own_l[it / 64] = lg[k];
+    }
+  }
+  if (tid < S && tid != split) {
+    const uint64_t* fl = a.flags + grp * S + tid;
+    uint32_t spins = 0;
+    while (__hip_atomic_load(fl, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != tag && ++spins < kFlagSpins)
+      __builtin_amdgcn_s_sleep(1);
+  }
+  __syncthreads();
+  if constexpr (G >= 2) {
+    if (spread)
+      merge_head<G, 64 * NW>(a, grp, S, split, (int)(tk - first), ob, lds.own_o, lds.own_l, lds.w, lds.red);
+    else
+      merge_tail<G, 64 * NW>(a, grp, S, split, ob, lds.own_o, lds.own_l, lds.w, lds.red);
+  } else {
+    merge_tail<G, 64 * NW>(a, grp, S, split, ob, lds.own_o, lds.own_l, lds.w, lds.red);
+  }
+  if (tk == (uint32_t)(S - 1) && tid == 0) {
+    __hip_atomic_store(a.counters + grp, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(a.epochs + grp, epoch + 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+
+
 // Split `split` of group (bb, hk) by a workgroup of NW waves: wave w takes
 // chunks w, w + NW, ... of the split. Every workgroup of the group writes its
 // partial (several splits) and the last one(s) to finish merge them.
@@ -650,85 +747,7 @@ __device__ __forceinline__ void decode_split(const DecodeArgs& a, int bb, int hk
       }
     }
   }
-  const size_t ob = (size_t)bb * a.q_heads + (size_t)hk * G;
-  if (single) {
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-      const int it = tid + k * NT2;
-      if (it < G * 64) {
-        *reinterpret_cast<f2_t*>(a.out + ob * kHeadDim + 2 * it) = val[k];
-        if (it % 64 == 0 && a.lse) a.lse[ob + it / 64] = lg[k] == ninf ? ninf : lg[k] * kLn2;
-      }
-    }
-    return;
-  }
-  if (tid == 0) lds.ticket = ticket;
-  lds_sync();
-  // The call count read at the start is first used here: it stays in a
-  // vector register until now, so no earlier instruction waits for it.
-  __asm__ volatile("" : "+v"(epoch));
-  // Merging splits: the one holding the last ticket, or with many splits
-  // those holding the last G tickets, one query head each. A ready flag
-  // carries this call's tag (the group's merged-call count + 1, and S), so
-  // flags left by earlier calls never match and no flag is ever reset; the
-  // split holding the last ticket returns the ticket counter to zero and
-  // advances the count once every ticket is taken.
-  const uint32_t tk = lds.ticket;
-  const bool spread = G >= 2 && S >= kSpreadSplits && S >= G;
-  const uint32_t first = spread ? (uint32_t)(S - G) : (uint32_t)(S - 1);
-  const uint64_t tag = ((uint64_t)(epoch + 1u) << 32) | (uint32_t)S;
-  if (spread || tk < first) {
-    // Publish: agent-scope stores write through to the level every L2 slice
-    // reads (sc1), every thread waits for their acknowledgement, then one
-    // thread raises the split's ready flag.
-    float* po = a.part_o + (grp * S + split) * (size_t)(G * kHeadDim);
-    float* pl = a.part_lse + (grp * S + split) * (size_t)G;
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-      const int it = tid + k * NT2;
-      if (it < G * 64) {
-        __hip_atomic_store(po + 2 * it, val[k].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(po + 2 * it + 1, val[k].y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (it % 64 == 0) __hip_atomic_store(pl + it / 64, lg[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
-    }
-    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) __hip_atomic_store(a.flags + grp * S + split, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (tk < first) return;
-  }
-
-  // Alg. 2, "Combine", in a merging split: its own partial stays in LDS;
-  // every other split has taken its ticket and is publishing (or has), so
-  // thread t < S waits for split t's flag (agent-scope loads), then the
-  // partials are read with agent-scope loads and merged.
-#pragma unroll
-  for (int k = 0; k < kItems; ++k) {
-    const int it = tid + k * NT2;
-    if (it < G * 64) {
-      *reinterpret_cast<f2_t*>(&lds.own_o[2 * it]) = val[k];
-      if (it % 64 == 0) lds.own_l[it / 64] = lg[k];
-    }
-  }
-  if (tid < S && tid != split) {
-    const uint64_t* fl = a.flags + grp * S + tid;
-    uint32_t spins = 0;
-    while (__hip_atomic_load(fl, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != tag && ++spins < kFlagSpins)
-      __builtin_amdgcn_s_sleep(1);
-  }
-  __syncthreads();
-  if constexpr (G >= 2) {
-    if (spread)
-      merge_head<G, 64 * NW>(a, grp, S, split, (int)(tk - first), ob, lds.own_o, lds.own_l, lds.w, lds.red);
-    else
-      merge_tail<G, 64 * NW>(a, grp, S, split, ob, lds.own_o, lds.own_l, lds.w, lds.red);
-  } else {
-    merge_tail<G, 64 * NW>(a, grp, S, split, ob, lds.own_o, lds.own_l, lds.w, lds.red);
-  }
-  if (tk == (uint32_t)(S - 1) && tid == 0) {
-    __hip_atomic_store(a.counters + grp, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(a.epochs + grp, epoch + 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
+  finish_split<G, NW>(a, grp, split, (size_t)bb * a.q_heads + (size_t)hk * G, ticket, epoch, val, lg, lds);
 }
 
 }  // namespace

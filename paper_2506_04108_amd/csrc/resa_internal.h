@@ -147,6 +147,43 @@ struct RectifyArgs {
   const int32_t* seq_mask;     // [B]: sequences with 0 are left untouched (null: every sequence)
 };
 
+// Packed rows into or out of an 8-bit cache.
+struct RowsQ8Args {
+  CacheArgs c;                 // k and v hold codes
+  float* k_scale;              // [B, Hkv, max_blocks], paged: [num_pages, Hkv]
+  float* v_scale;
+  int32_t format;
+  const uint16_t* k_rows;      // [rows, Hkv, D] with k_stride elements from row to row
+  const uint16_t* v_rows;
+  int64_t k_stride, v_stride;
+  uint16_t* k_out;             // [rows, Hkv, D], contiguous
+  uint16_t* v_out;
+  const int32_t* cu;           // [B + 1]: sequence s has rows [cu[s], cu[s + 1])
+  int32_t rows;
+  const int32_t* seq_lens;
+};
+
+// Attention of packed rows: over their own packed keys (prompts), or over an
+// 8-bit cache whose last rows they are.
+struct RowsArgs {
+  CacheArgs c;                 // 8-bit cache
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* seq_lens;
+  const uint16_t* q;           // [rows, Hq, D] with q_stride elements from row to row
+  const uint16_t* k;           // prompts: [rows, Hkv, D] with k_stride, v_stride
+  const uint16_t* v;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t* cu;           // [batch + 1]
+  int32_t batch, rows, q_heads, kv_heads, group;
+  int32_t chunk, num_splits;   // keys per split, splits
+  float scale_log2;
+  uint16_t* out;               // [rows, Hq, D]
+  float* lse;                  // [rows, Hq] or null
+  float* part_o;               // [num_splits, rows, Hq, D]
+  float* part_lse;             // [num_splits, rows, Hq]
+};
+
 // Launchers: enqueue on `stream`; return the hipError_t of the launch.
 hipError_t launch_summarize(const CacheArgs& c, const int32_t* seq_lens, int32_t blk_begin,
                             int32_t blk_end, hipStream_t stream);
@@ -155,6 +192,12 @@ hipError_t launch_append(const CacheArgs& c, const uint16_t* k_new, const uint16
 hipError_t launch_select(const SelectArgs& a, hipStream_t stream);
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t stream);
 hipError_t launch_rectify(const RectifyArgs& a, hipStream_t stream);
+hipError_t launch_store_rows_q8(const RowsQ8Args& a, hipStream_t stream);
+hipError_t launch_load_rows_q8(const RowsQ8Args& a, hipStream_t stream);
+hipError_t launch_decode_q8(const DecodeArgs& a, const float* k_scale, const float* v_scale, int32_t format,
+                            hipStream_t stream);
+hipError_t launch_rows_q8(const RowsArgs& a, int32_t format, hipStream_t stream);
+hipError_t launch_prompt(const RowsArgs& a, hipStream_t stream);
 hipError_t launch_clear(void* p, size_t bytes, hipStream_t stream);
 hipError_t launch_stream_read(const void* buf, size_t bytes, uint32_t* sink, uint32_t match,
                               int32_t workgroups, hipStream_t stream);
@@ -164,6 +207,10 @@ int32_t select_fused_max_blocks();
 int32_t select_blocks_per_wg(int32_t batch, int32_t kv_heads, int32_t max_blocks_seq);
 int32_t select_hist_words(int32_t batch, int32_t kv_heads, int32_t max_blocks_seq);
 int32_t decode_auto_splits(int32_t batch, int32_t kv_heads, int32_t n_cap, int32_t block_size);
+int32_t decode_q8_auto_splits(int32_t batch, int32_t kv_heads, int32_t n_cap, int32_t block_size);
+int32_t rows_waves(int32_t batch, int32_t rows, int32_t group);
+int32_t rows_chunk(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len);
+int32_t rows_max_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len);
 int32_t rectify_num_qblocks(int32_t group, int32_t f);
 int32_t rectify_chunk(int32_t batch, int32_t kv_heads, int32_t rows, int32_t max_seq_len, bool masked);
 int32_t rectify_ref_keys(int32_t batch, int32_t kv_heads, int32_t rows, int32_t max_seq_len);

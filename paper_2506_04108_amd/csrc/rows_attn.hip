@@ -1,0 +1,830 @@
+// Dense causal attention of packed query rows on gfx950 matrix cores: whole
+// prompts of different lengths over their own keys (bf16), and the last rows
+// of each sequence over an 8-bit cache (rectification, chunked prefill).
+//
+// Row rho = r * g + h of a (sequence, kv head) group is head h of the
+// sequence's packed row r, at position L - n + r; it sees keys up to there. A
+// workgroup takes 32 kWaves consecutive rows (a query block) and one split of
+// the keys, each wave 32 rows, and walks the keys tile by tile:
+//   S^T = K . Q^T     v_mfma_f32_32x32x16_bf16 (keys x queries): lane l holds
+//                     query l % 32 and keys 8 (i / 4) + 4 (l / 32) + i % 4,
+//                     i = 0 .. 15, of each 32
+//   weights           2^(S c - m), fp32; their sum is of the fp32 values
+//   O^T += V^T . P^T  v_mfma_f32_32x32x16_bf16 (dims x queries), with the
+//                     contraction in the order in which the lanes hold the
+//                     weights; V^T through the LDS transpose read
+// The weights enter the second product as bf16 (8 significant bits, error at
+// most 2^-9 each, independent from key to key): the result is rounded to bf16
+// itself, and with bf16 operands no V is out of range and V needs no
+// conversion, so that K and V rows go from HBM straight into LDS. (With fp16
+// weights, V converted on its way and a second pass for what fp16 cannot hold,
+// the bf16 cache's rectification runs at 1.02 - 1.16 PFLOP/s.)
+//
+// A tile's weights are formed while the matrix cores produce the scores of the
+// next one (two MFMAs, then the VALU work of a few weights, kept in that order
+// by scheduling barriers), then its P.V runs. One barrier per two tiles. The
+// softmax reference is the maximum of the first tile and moves only when the
+// weights of a tile sum to more than 2^12 over a lane's keys, so that no tile
+// needs its maximum beforehand.
+//
+// The query blocks are dealt longest first (every workgroup finds its own by
+// a search over the sequences' counts, in one wave's registers), with the kv
+// heads of a block next to each other: workgroups go to the 8 XCDs in turn,
+// so that with 8 kv heads the blocks of one head share an L2.
+//
+// 8-bit cache: the codes are bf16 values, so both products are on the codes
+// themselves; a block's key scale multiplies the score (inside the fma of the
+// weight) and its value scale the weight. Codes go through registers, a
+// conversion per workgroup, into the same LDS tiles.
+//
+// Masked keys: scores are replaced, so nothing of a masked K row matters; a
+// masked V row meets weights of zero, which only a value that is not finite
+// would survive. The tiles that some row of the workgroup masks are searched
+// for such values, and a workgroup that finds one takes its range again, a
+// tile at a time, with these values apart.
+#include <type_traits>
+
+#include "rows_device.h"
+
+namespace resa {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kRowsPerWave = 32;
+constexpr int kLoadRows = 8;               // tile rows whose K and V each wave brings in
+constexpr int kRowBytes = kHeadDim * 2;
+constexpr int kCus = 256;
+constexpr float kMaxWeightSum = 4096.f;
+constexpr int kPacked = -1;                // source of keys: packed bf16 rows, else the format of the 8-bit cache
+
+// Rows of a tile are 256 B; 16-byte piece p of row r sits in slot p ^ swz(r),
+// which keeps both the K reads (16 rows, one piece) and the V transpose reads
+// (4 aligned rows, four neighbouring pieces) free of bank conflicts.
+__host__ __device__ constexpr int swz(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
+
+constexpr int kWaitVm0 = 0x0F70, kWaitLgkm0 = 0xC07F;
+
+__device__ __forceinline__ i32x4_t rsrc_words(const void* p, int bytes) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  return i32x4_t{(int32_t)__builtin_amdgcn_readfirstlane((uint32_t)u),
+                 (int32_t)(__builtin_amdgcn_readfirstlane((uint32_t)(u >> 32)) & 0xffffu),
+                 __builtin_amdgcn_readfirstlane(bytes), kBufWord3};
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(wave_uniform(const_cast<void*>(p)), (short)0,
+                                           __builtin_amdgcn_readfirstlane(bytes), kBufWord3);
+}
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+// A wave's eight rows of a tile straight into LDS: lane i's 16 bytes at offset
+// voff0 (voff1) of the resource land at lds + 16 i (lds + 1024 + 16 i). The
+// completion is ordered by hand (vmcnt 0, then a barrier). M0 is restored.
+__device__ __forceinline__ void lds_load_rows8(uint32_t lds, uint32_t voff0, uint32_t voff1, i32x4_t rk) {
+  uint32_t saved;
+  __asm__ volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+      "s_add_i32 m0, %1, 1024\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved) : "s"(lds), "v"(voff0), "v"(voff1), "s"(rk) : "memory", "scc");
+}
+__device__ __forceinline__ void compiler_fence() { __asm__ volatile("" ::: "memory"); }
+__device__ __forceinline__ void bare_barrier() {
+  compiler_fence();
+  __builtin_amdgcn_s_barrier();
+  compiler_fence();
+}
+__device__ __forceinline__ f32x16_t mfma32(bf16x8_t a, bf16x8_t b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16_t mfma32(f16x8_t a, f16x8_t b, f32x16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+// x - y, the product x rounded first (never contracted to one operation).
+__device__ __forceinline__ float sub_rounded(float x, float y) {
+  __asm__ volatile("" : "+v"(x));
+  return x - y;
+}
+__device__ __forceinline__ bool finite_f(float x) { return fabsf(x) < __builtin_inff(); }
+// Whether one of the two bf16 values of a word is infinite or NaN.
+__device__ __forceinline__ bool not_finite2(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+__device__ __forceinline__ uint32_t finite_or_0(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+}
+
+// Rows of a sequence as a launch sees them: n rows from packed row `first` on,
+// the last of L keys; n = 0 where the call leaves the sequence out.
+struct SeqRows {
+  int first, n, L;
+};
+template <int kSrc>
+__device__ __forceinline__ SeqRows seq_rows(const RowsArgs& a, int s) {
+  SeqRows q;
+  packed_rows(a.cu, a.rows, s, q.first, q.n);
+  q.L = kSrc == kPacked ? q.n : a.seq_lens[s];
+  if (kSrc != kPacked && (q.L < q.n || q.L > a.c.capacity)) q.n = 0;
+  return q;
+}
+
+// Query block `item`, longest first. A block's cost is its last row's position
+// in units of a block's rows: block b of a sequence with h rows' worth of
+// earlier keys costs h + b + 1. The cost of item i is the largest x with more
+// than i blocks of cost >= x; among the blocks of that cost the sequences come
+// in order.
+template <int kSrc>
+__device__ __forceinline__ bool find_block(const RowsArgs& a, int item, int per, int& seq, int& qblk) {
+  const int lane = threadIdx.x & 63;
+  const int G = a.group;
+  auto blocks = [&](int s, int& h) -> int {
+    h = 0;
+    if (s >= a.batch) return 0;
+    const SeqRows q = seq_rows<kSrc>(a, s);
+    if (kSrc != kPacked) h = (int)((int64_t)(q.L - q.n) * G / per);
+    return (int)(((int64_t)q.n * G + per - 1) / per);
+  };
+  int h0;
+  const int nb0 = blocks(lane, h0);  // the first 64 sequences' stay in registers
+  auto at_least = [&](int x) -> int {  // blocks of cost >= x
+    int c = min(max(h0 + nb0 - x + 1, 0), nb0);
+    for (int base = 64; base < a.batch; base += 64) {
+      int h;
+      const int nb = blocks(base + lane, h);
+      c += min(max(h + nb - x + 1, 0), nb);
+    }
+    return wave_total(c);
+  };
+  int most = h0 + nb0;
+  for (int base = 64; base < a.batch; base += 64) {
+    int h;
+    const int nb = blocks(base + lane, h);
+    most = max(most, h + nb);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) most = max(most, __shfl_xor(most, d));
+  most = __builtin_amdgcn_readfirstlane(most);
+  if (at_least(1) <= item) return false;
+  int lo = 1, hi = most + 1;  // more than `item` blocks of cost >= lo, not of cost >= hi
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (at_least(mid) > item) lo = mid;
+    else hi = mid;
+  }
+  int rank;
+  auto of_cost = [&](int s) -> int {
+    int h;
+    const int nb = blocks(s, h);
+    return lo > h && lo <= h + nb ? 1 : 0;
+  };
+  if (!find_seq(item - at_least(lo + 1), a.batch, of_cost, seq, rank)) return false;
+  int h;
+  blocks(seq, h);
+  qblk = lo - h - 1;
+  return true;
+}
+
+template <int kWaves, int kSrc, bool kPaged>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_rows_attn(RowsArgs a) {
+  constexpr bool kQ8 = kSrc != kPacked;
+  // Weights and V: bf16, or over codes fp16.
+  typedef std::conditional_t<kQ8, f16x8_t, bf16x8_t> P8;
+  constexpr int kKT = kLoadRows * kWaves;  // keys per tile
+  constexpr int kKT32 = kKT / 32, kKT16 = kKT / 16;
+  constexpr int kRowsPerWg = kRowsPerWave * kWaves;
+  constexpr int kTileBytes = kKT * kRowBytes;
+  struct Lds {
+    uint8_t k[4][kTileBytes];    // tile t in stage t % 4
+    uint8_t v[4][kTileBytes];
+    float fk[4][4], fv[4][4];    // 8-bit cache: factors of each 16 keys (scores, weights)
+    int odd;                     // a masked tile holds a V value that is not finite
+  };
+  __shared__ __attribute__((aligned(1024))) Lds lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hk = blockIdx.x % a.kv_heads;
+  const int S = a.num_splits;
+  const int rest = blockIdx.x / a.kv_heads;
+  const int split = rest % S;
+  int seq, qblk;
+  if (!find_block<kSrc>(a, rest / S, kRowsPerWg, seq, qblk)) return;
+  const SeqRows sr = seq_rows<kSrc>(a, seq);
+  const int G = a.group, R = sr.n * G, past = sr.L - sr.n;
+  const int k0 = split * a.chunk;
+  const int last_row = min(R - 1, (qblk + 1) * kRowsPerWg - 1);
+  const int k1 = min(min(k0 + a.chunk, sr.L), past + last_row / G + 1);
+  if (k1 <= k0) return;  // no key of this split is seen: the merge does not read it
+  const int ntiles = (k1 - k0 + kKT - 1) / kKT;
+  const float ninf = -__builtin_inff();
+  // Softmax scale: a negative one negates the queries, zero clears them.
+  const float c = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+  const uint32_t q_and = a.scale_log2 == 0.f ? 0u : ~0u, q_xor = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+  const int hi = lane >> 5, lq = lane & 31;
+  const int row_base = qblk * kRowsPerWg + wave * kRowsPerWave;
+  const int rho = row_base + lq;
+  // Keys past lim are masked. Rows past the last one follow it (their queries
+  // are zero and nothing of theirs is stored).
+  const int lim = min(past + min(rho, R - 1) / G, k1 - 1);
+  // Tiles that reach past `cut` (of the wave) or `wg_cut` (of any wave) mask
+  // something.
+  const int cut = min(k1, past + min(row_base, R - 1) / G);
+  const int wg_cut = past + qblk * kRowsPerWg / G;
+
+  // Packed rows straight into LDS: lane i fills slot i % 16 of rows wrow +
+  // i / 16 and + 4, fetching the row's piece (i % 16) ^ swz(row).
+  const int wrow = kLoadRows * wave;
+  const int lrow = lane >> 4, lslot = lane & 15;
+  uint32_t koff[2], voff[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const uint32_t piece = 16 * (lslot ^ swz(wrow + 4 * e + lrow));
+    koff[e] = (uint32_t)(4 * e + lrow) * (uint32_t)(2 * a.k_stride) + piece;
+    voff[e] = (uint32_t)(4 * e + lrow) * (uint32_t)(2 * a.v_stride) + piece;
+  }
+  const uint32_t lds0 = lds_addr(&lds);
+  const uint32_t lds_k = __builtin_amdgcn_readfirstlane(lds0) + (uint32_t)(wrow * kRowBytes);
+  // LDS read addresses (stage, 32-key part and k-step of P.V are immediates).
+  // K: row lq, piece (2 ks + hi) ^ swz(lq). V^T by transpose reads, lane c of
+  // 16 passing the address of key c / 4, dims 4 (c % 4) .. ; eight rows further
+  // the slots differ in bit 1. The pieces of k-step ks and of dims 32 dt are an
+  // exclusive or with 32 ks and 64 dt, taken once a round: held in registers
+  // they made the 8-wave kernels spill.
+  uint32_t kbase = lds0 + lq * kRowBytes + 16 * (hi ^ swz(lq));
+  uint32_t vbase;
+  {
+    const int vr = 4 * hi + ((lane & 15) >> 2);
+    const int vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    vbase = lds0 + (uint32_t)offsetof(Lds, v) + vr * kRowBytes + 16 * (vpiece ^ swz(vr)) + 8 * (lane & 1);
+  }
+  auto fresh = [](uint32_t& x) __attribute__((always_inline)) { __asm__ volatile("" : "+v"(x)); };
+  typedef __attribute__((address_space(3))) const bf16x8_t lds_bf16x8;
+  typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+  auto read_k = [&](int st, int ks, bf16x8_t (&ka)[kKT32]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kt = 0; kt < kKT32; ++kt)
+      ka[kt] = *(lds_bf16x8*)(uintptr_t)((kbase ^ (32 * ks)) + st * kTileBytes + kt * 32 * kRowBytes);
+  };
+  auto read_v32 = [&](int st, int ks, int dt) __attribute__((always_inline)) -> P8 {
+    i16x4_t x[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_i16x4*)(uintptr_t)((vbase ^ (64 * dt + 32 * e)) + 8 * e * kRowBytes + st * kTileBytes + 16 * ks * kRowBytes));
+    return __builtin_bit_cast(P8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto read_v = [&](int st, int ks, P8 (&va)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) va[dt] = read_v32(st, ks, dt);
+  };
+
+  // Q^T (B of S^T): lane holds row lq, dims 16 s + 8 hi .. + 8 for k-step s.
+  bf16x8_t qb[8];
+  {
+    const int h = rho % G, r = rho / G;
+    const uint16_t* qp = a.q + (int64_t)(sr.first + min(r, sr.n - 1)) * a.q_stride + (hk * G + h) * kHeadDim + 8 * hi;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      U4 x = ld16(qp + 16 * s);
+      if (rho >= R) x = U4{0, 0, 0, 0};
+      qb[s] = __builtin_bit_cast(bf16x8_t, U4{(x.x & q_and) ^ q_xor, (x.y & q_and) ^ q_xor,
+                                             (x.z & q_and) ^ q_xor, (x.w & q_and) ^ q_xor});
+    }
+  }
+
+  // This wave's rows of tile ti: how many exist below k1.
+  auto rows_of = [&](int ti) __attribute__((always_inline)) -> int {
+    return min(max(k1 - (k0 + ti * kKT + wrow), 0), kLoadRows);
+  };
+  // Packed keys: K and V of a tile, requested straight into their stages.
+  auto issue_packed = [&](const uint16_t* p, int64_t stride, const uint32_t (&off)[2], uint32_t to, int ti)
+                          __attribute__((always_inline)) {
+    const int have = rows_of(ti);
+    const int nrec = have > 0 ? (have - 1) * (int)(2 * stride) + kRowBytes : 0;
+    lds_load_rows8(to, off[0], off[1],
+                   rsrc_words(p + (int64_t)(sr.first + k0 + ti * kKT + wrow) * stride + hk * kHeadDim, nrec));
+  };
+  auto issue_k = [&](int ti, int st) __attribute__((always_inline)) {
+    issue_packed(a.k, a.k_stride, koff, lds_k + (uint32_t)(st * kTileBytes), ti);
+  };
+  auto issue_v = [&](int ti, int st) __attribute__((always_inline)) {
+    issue_packed(a.v, a.v_stride, voff, lds_k + (uint32_t)(offsetof(Lds, v) + st * kTileBytes), ti);
+  };
+  // 8-bit cache: the wave's eight rows of a tile (they lie in one block) are
+  // 1 KB, 16 codes of row lane / 8 a lane, held until they are converted.
+  struct Codes {
+    U4 x;
+    float ks, vs;
+  };
+  auto ask = [&](bool key, int ti) __attribute__((always_inline)) -> Codes {
+    Codes w;
+    const int at = k0 + ti * kKT + wrow;
+    int have = rows_of(ti);
+    const int m = min(at >> a.c.log2_block, a.c.max_blocks - 1);
+    int64_t row, si;
+    if constexpr (kPaged) {
+      const int page = __builtin_amdgcn_readfirstlane(a.c.table[(size_t)seq * a.c.max_blocks + m]);
+      if ((unsigned)page >= (unsigned)a.c.num_pages) have = 0;
+      const int64_t p = have > 0 ? page : 0;
+      si = p * a.c.kv_heads + hk;
+      row = si * a.c.block_size + (at & (a.c.block_size - 1));
+    } else {
+      const int64_t grp = (int64_t)seq * a.c.kv_heads + hk;
+      si = grp * a.c.max_blocks + m;
+      row = grp * a.c.capacity + at;
+    }
+    const uint8_t* base = reinterpret_cast<const uint8_t*>(key ? a.c.k : a.c.v);
+    const __amdgpu_buffer_rsrc_t rx = uniform_rsrc(base + row * kHeadDim, have * kHeadDim);
+    w.x = __builtin_bit_cast(U4, __builtin_amdgcn_raw_buffer_load_b128(rx, 16 * lane, 0, 0));
+    const __amdgpu_buffer_rsrc_t rv = uniform_rsrc(a.v_scale + si, 4);
+    w.vs = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rv, 0, 0, 0));
+    w.ks = 0.f;
+    if (key) {
+      const __amdgpu_buffer_rsrc_t rk = uniform_rsrc(a.k_scale + si, 4);
+      w.ks = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rk, 0, 0, 0));
+    }
+    return w;
+  };
+  // Converted into the tile's stage. A block with a scale that is no finite
+  // number (it was made of rows that held one) has NaN for its keys: whoever
+  // sees it gets NaN, and for the others its V counts as zero.
+  auto put = [&](bool key, const Codes& w, int st) __attribute__((always_inline)) {
+    if constexpr (kQ8) {
+      const bool odd = !finite_f(w.vs) || (key && !finite_f(w.ks));
+      uint32_t h[8];
+      const uint32_t in[4] = {w.x.x, w.x.y, w.x.z, w.x.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kSrc == RESA_Q8_INT8) {
+          float y[4];
+          codes_f32<kSrc>(in[i], y);
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            h[2 * i + u] = key ? __builtin_amdgcn_perm(__float_as_uint(y[2 * u + 1]), __float_as_uint(y[2 * u]), 0x07060302u)
+                               : __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)y[2 * u], (_Float16)y[2 * u + 1]});
+        } else if (key) {
+          h[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in[i], 1.f, false));
+          h[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in[i], 1.f, true));
+        } else {
+          h[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[i], 1.f, false));
+          h[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[i], 1.f, true));
+        }
+      }
+      if (__builtin_expect(__any(odd), 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = key ? 0x7fc07fc0u : 0u;
+      }
+      const int row = wrow + (lane >> 3), piece = 2 * (lane & 7);
+      uint8_t* tile = key ? lds.k[st] : lds.v[st];
+      st16(tile + row * kRowBytes + 16 * (piece ^ swz(row)), U4{h[0], h[1], h[2], h[3]});
+      st16(tile + row * kRowBytes + 16 * ((piece + 1) ^ swz(row)), U4{h[4], h[5], h[6], h[7]});
+      if ((wave & 1) == 0 && lane == 0) {
+        if (key) lds.fk[st][wave >> 1] = odd ? c : w.ks * c;
+        else lds.fv[st][wave >> 1] = odd ? 0.f : w.vs;
+      }
+    }
+  };
+
+  f32x16_t o[4];
+  auto clear_o = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+  };
+  clear_o();
+  float m = ninf, l = 0.f;  // l: over this lane's keys; summed across the two halves at the end
+  bool guard = false;       // second pass, V values that are not finite left out
+
+  auto mask = [&](int t0, f32x16_t (&s)[kKT32]) __attribute__((always_inline)) {
+    const int d = lim - t0 - 4 * hi;
+#pragma unroll
+    for (int kt = 0; kt < kKT32; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kt][i] = 32 * kt + 8 * (i >> 2) + (i & 3) > d ? ninf : s[kt][i];
+  };
+  // Factors of a tile's scores and of its weights, for each 16 keys. Those of
+  // the scores are read with the K they belong to, a round before their use.
+  struct Factors {
+    float x[kKT16];
+  };
+  auto key_factors = [&](int st) __attribute__((always_inline)) -> Factors {
+    Factors f;
+#pragma unroll
+    for (int i = 0; i < kKT16; ++i) f.x[i] = kQ8 ? lds.fk[st][i] : c;
+    return f;
+  };
+  // fp16 weights carry the value scale over vref, a power of two above the
+  // largest value scale met so far, which the accumulators are in units of.
+  float vref = 0x1p-126f;
+  auto value_factors = [&](int st) __attribute__((always_inline)) -> Factors {
+    Factors f;
+    if constexpr (kQ8) {
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < kKT16; ++i) {
+        f.x[i] = lds.fv[st][i];
+        top = fmaxf(top, f.x[i]);
+      }
+      if (__builtin_expect(__any(top > vref), 0)) {
+        const float up = __uint_as_float((__float_as_uint(top) & 0x7f800000u) + 0x00800000u);
+        const float alpha = vref / up;
+        vref = up;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
+      }
+      const float inv = 1.f / vref;
+#pragma unroll
+      for (int i = 0; i < kKT16; ++i) f.x[i] *= inv;
+    }
+    return f;
+  };
+  auto row_max = [&](const f32x16_t (&s)[kKT32], const Factors& f) __attribute__((always_inline)) {
+    float x = ninf;
+#pragma unroll
+    for (int kt = 0; kt < kKT32; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x = fmaxf(x, s[kt][i] * f.x[2 * kt + (i >> 3)]);
+    return max_xor32(x);
+  };
+  auto weight = [&](float y, int i, const Factors& g, P8 (&ph)[kKT16], float (&ps)[4]) __attribute__((always_inline)) {
+    const float pe = fast_exp2(y);
+    ps[i & 3] += pe;
+    if constexpr (kQ8)
+      ph[i >> 3][i & 7] = (_Float16)(pe * g.x[i >> 3]);
+    else
+      ph[i >> 3][i & 7] = (__bf16)pe;
+  };
+  auto scores = [&](int st, f32x16_t (&s)[kKT32]) __attribute__((always_inline)) {
+    bf16x8_t ka[kKT32];
+#pragma unroll
+    for (int kt = 0; kt < kKT32; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      read_k(st, ks, ka);
+#pragma unroll
+      for (int kt = 0; kt < kKT32; ++kt) s[kt] = mfma32(ka[kt], qb[ks], s[kt]);
+    }
+  };
+  // Weights of one tile (scores s) interleaved with the scores of the next
+  // (K stage st, into sn).
+  auto weights_scores = [&](auto stage, const f32x16_t (&s)[kKT32], f32x16_t (&sn)[kKT32], const Factors& f,
+                            const Factors& g, P8 (&ph)[kKT16]) __attribute__((always_inline)) {
+    constexpr int st = decltype(stage)::value;
+    float ps[4] = {0.f, 0.f, 0.f, 0.f};
+    bf16x8_t ka[2][kKT32];
+    read_k(st, 0, ka[0]);
+#pragma unroll
+    for (int kt = 0; kt < kKT32; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sn[kt][i] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      if (ks < 7) read_k(st, ks + 1, ka[(ks + 1) & 1]);
+#pragma unroll
+      for (int kt = 0; kt < kKT32; ++kt) sn[kt] = mfma32(ka[ks & 1][kt], qb[ks], sn[kt]);
+#pragma unroll
+      for (int i = 2 * kKT32 * ks; i < 2 * kKT32 * (ks + 1); ++i) weight(fmaf(s[i >> 4][i & 15], f.x[i >> 3], -m), i, g, ph, ps);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    return (ps[0] + ps[1]) + (ps[2] + ps[3]);
+  };
+  Codes held[2];
+  // One tile: its weights (scores s) with the next tile's scores (sn), then
+  // its P.V.
+  //
+  // Order between the waves, with a barrier before every even tile 2p only.
+  // Rounds 2p and 2p + 1 read K(2p + 1), K(2p + 2), V(2p) and V(2p + 1). After
+  // the barrier the stages of K(2p - 1), K(2p), V(2p - 2) and V(2p - 1) are
+  // free (last read in rounds 2p - 2 and 2p - 1); K(2p + 3), K(2p + 4),
+  // V(2p + 2) and V(2p + 3) are requested into them, and are there at the next
+  // barrier, before which every wave has waited for its own.
+  auto round = [&](int ti, auto stage, f32x16_t (&s)[kKT32], f32x16_t (&sn)[kKT32], const Factors& f,
+                   Factors& fn) __attribute__((always_inline)) {
+    constexpr int st = decltype(stage)::value;
+    const int t0 = k0 + ti * kKT;
+    if constexpr (st % 2 == 0) {
+      __builtin_amdgcn_s_waitcnt(kWaitVm0);
+      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+      bare_barrier();
+      if constexpr (!kQ8) {
+        issue_k(ti + 3, (st + 3) & 3);
+        issue_k(ti + 4, st);
+        issue_v(ti + 2, (st + 2) & 3);
+        issue_v(ti + 3, (st + 3) & 3);
+      }
+    }
+    // Codes: the two K tiles in the even round, the two V tiles in the odd.
+    if constexpr (kQ8) {
+      constexpr int ahead = st % 2 == 0 ? 3 : 1;
+      held[0] = ask(st % 2 == 0, ti + ahead);
+      held[1] = ask(st % 2 == 0, ti + ahead + 1);
+    }
+    if constexpr (!kQ8) {
+      // What this wave brought of a tile that some row masks: any value that
+      // is not finite? In the second pass such values are cleared.
+      if (__builtin_expect(guard || t0 + kKT > wg_cut, 0)) {
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          uint8_t* at = lds.v[st] + (wrow + 4 * e) * kRowBytes + 16 * lane;
+          const U4 x = ld16(at);
+          const bool some = not_finite2(x.x) || not_finite2(x.y) || not_finite2(x.z) || not_finite2(x.w);
+          if (guard && some) st16(at, U4{finite_or_0(x.x), finite_or_0(x.y), finite_or_0(x.z), finite_or_0(x.w)});
+          odd = odd || some;
+        }
+        if (__any(odd)) lds.odd = 1;
+        if (guard) {
+          __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+          bare_barrier();
+        }
+      }
+    }
+    const Factors g = value_factors(st);
+    fn = key_factors((st + 1) & 3);
+    P8 ph[kKT16];
+    fresh(kbase);
+    __builtin_amdgcn_sched_barrier(0);
+    float ps = weights_scores(std::integral_constant<int, (st + 1) & 3>{}, s, sn, f, g, ph);
+    // Rare: move the reference and form the weights again. A row without one
+    // so far (no tile with a finite score) takes this branch too.
+    if (__builtin_expect(__any(!(ps <= kMaxWeightSum)), 0)) {
+      const float mn = fmaxf(m, row_max(s, f));
+      const float alpha = m == mn ? 1.f : fast_exp2(m - mn);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
+      const float mref = m == ninf ? 0.f : m;
+      float pt[4] = {0.f, 0.f, 0.f, 0.f};
+      // From the rounded logits that the reference is the maximum of: with
+      // logits past 2^31 the unrounded product may exceed it by hundreds.
+#pragma unroll
+      for (int i = 0; i < 16 * kKT32; ++i) weight(sub_rounded(s[i >> 4][i & 15] * f.x[i >> 3], mref), i, g, ph, pt);
+      ps = (pt[0] + pt[1]) + (pt[2] + pt[3]);
+    }
+    l += ps;
+    if (__builtin_expect(t0 + 2 * kKT > cut, 0)) mask(t0 + kKT, sn);
+    __builtin_amdgcn_sched_barrier(0);
+    P8 va[2][4];
+    fresh(vbase);
+    read_v(st, 0, va[0]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < kKT16; ++ks) {
+      if (ks < kKT16 - 1) read_v(st, ks + 1, va[(ks + 1) & 1]);
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) o[dt] = mfma32(va[ks & 1][dt], ph[ks], o[dt]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (kQ8) {
+      constexpr int ahead = st % 2 == 0 ? 3 : 1;
+      put(st % 2 == 0, held[0], (st + ahead) & 3);
+      put(st % 2 == 0, held[1], (st + ahead + 1) & 3);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  if (tid == 0) lds.odd = 0;
+  for (;;) {
+    if constexpr (kQ8) {
+      const Codes first[5] = {ask(true, 0), ask(true, 1), ask(true, 2), ask(false, 0), ask(false, 1)};
+#pragma unroll
+      for (int t = 0; t < 3; ++t) put(true, first[t], t);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) put(false, first[3 + t], t);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 3; ++t) issue_k(t, t);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) issue_v(t, t);
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    bare_barrier();
+    f32x16_t sa[kKT32], sb[kKT32];
+    scores(0, sa);
+    if (k0 + kKT > cut) mask(k0, sa);
+    Factors fa = key_factors(0), fb;
+    m = row_max(sa, fa);
+    for (int ti = 0; ti < ntiles; ti += 4) {
+      round(ti, std::integral_constant<int, 0>{}, sa, sb, fa, fb);
+      if (ti + 1 >= ntiles) break;
+      round(ti + 1, std::integral_constant<int, 1>{}, sb, sa, fb, fa);
+      if (ti + 2 >= ntiles) break;
+      round(ti + 2, std::integral_constant<int, 2>{}, sa, sb, fa, fb);
+      if (ti + 3 >= ntiles) break;
+      round(ti + 3, std::integral_constant<int, 3>{}, sb, sa, fb, fa);
+    }
+    // No load may still be writing LDS when the workgroup ends or starts over.
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    bare_barrier();
+    if (kQ8 || guard || __builtin_expect(lds.odd == 0, 1)) break;
+    guard = true;
+    clear_o();
+    l = 0.f;
+  }
+
+  // V values that are not finite, cleared in the second pass: whoever sees
+  // one gets it added. Lane (r, c) looks at 16 bytes of rows r, r + 4, ...
+  if constexpr (!kQ8) {
+    if (__builtin_expect(guard, 0)) {
+      const uint16_t* vb = a.v + (int64_t)sr.first * a.v_stride + hk * kHeadDim;
+#pragma unroll 1
+      for (int t = k0; t < k1; t += 4) {
+        const int mine = t + lrow;
+        const U4 x = ld16(vb + (int64_t)min(mine, k1 - 1) * a.v_stride + 8 * lslot);
+        uint64_t who = __ballot(mine < k1 && (not_finite2(x.x) || not_finite2(x.y) || not_finite2(x.z) || not_finite2(x.w)));
+#pragma unroll 1
+        while (who != 0) {
+          const int r = __builtin_ctzll(who) >> 4;
+          who &= ~(0xffffull << (16 * r));
+          const uint16_t* vp = vb + (int64_t)(t + r) * a.v_stride + 4 * hi;
+          const bool see = t + r <= lim;
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + 32 * dt + 8 * (i >> 2) + (i & 3));
+              o[dt][i] += see && !finite_f(bf_lo(w)) ? bf_lo(w) : 0.f;
+              o[dt][i + 1] += see && !finite_f(bf_hi(w)) ? bf_hi(w) : 0.f;
+            }
+        }
+      }
+    }
+  }
+
+  const float lt = sum_xor32(l);
+  const float inv = lt == 0.f ? 0.f : (kQ8 ? vref : 1.f) / lt;
+  if (rho >= R) return;
+  const int row = sr.first + rho / G, head = hk * G + rho % G;
+  const size_t oi = (size_t)row * a.q_heads + head;
+  const float l2 = lt == 0.f ? ninf : m + fast_log2(lt);
+  if (S > 1) {
+    const size_t pi = (size_t)split * a.rows * a.q_heads + oi;
+    float* po = a.part_o + pi * kHeadDim;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4)
+        *reinterpret_cast<f32x4_t*>(po + 32 * dt + 8 * i4 + 4 * hi) =
+            f32x4_t{o[dt][4 * i4] * inv, o[dt][4 * i4 + 1] * inv, o[dt][4 * i4 + 2] * inv, o[dt][4 * i4 + 3] * inv};
+    if (hi == 0) a.part_lse[pi] = l2;
+    return;
+  }
+  // Lane (lq, hi) holds dims 32 dt + 8 i4 + 4 hi .. + 4 of its row: a lane
+  // swap gives hi = 0 the eight dims of i4 and hi = 1 those of i4 + 1.
+  uint16_t* out = a.out + oi * kHeadDim;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; i4 += 2) {
+      uint32_t x[2][2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          x[e][u] = pack_bf16(o[dt][4 * (i4 + e) + 2 * u] * inv, o[dt][4 * (i4 + e) + 2 * u + 1] * inv);
+      const auto s0 = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+      const auto s1 = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+      st16(out + 32 * dt + 8 * i4 + 8 * hi, U4{s0[0], s1[0], s0[1], s1[1]});
+    }
+  if (hi == 0 && a.lse) a.lse[oi] = lt == 0.f ? ninf : l2 * kLn2;
+}
+
+// Log-sum-exp merge of the splits (Alg. 2, "Combine"): a wave per (row, query
+// head), lane i holding dims 2 i and 2 i + 1. A row reads the splits that hold
+// keys it sees; rows of no sequence are left as they are.
+template <int kSrc>
+__global__ __launch_bounds__(256) void k_rows_combine(RowsArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t oi = (int64_t)blockIdx.x * 4 + wave;
+  const int row = (int)(oi / a.q_heads);
+  if (row >= a.rows) return;
+  // The sequence whose packed rows hold this row.
+  int seq = -1;
+  for (int base = 0; base < a.batch && seq < 0; base += 64) {
+    bool mine = false;
+    if (base + lane < a.batch) {
+      const SeqRows q = seq_rows<kSrc>(a, base + lane);
+      mine = row >= q.first && row < q.first + q.n;
+    }
+    const uint64_t who = __ballot(mine);
+    if (who != 0) seq = base + __builtin_ctzll(who);
+  }
+  if (seq < 0) return;
+  const SeqRows sr = seq_rows<kSrc>(a, seq);
+  const int keys = sr.L - sr.n + (row - sr.first) + 1;
+  const int n = min((keys + a.chunk - 1) / a.chunk, a.num_splits);
+  const size_t stride = (size_t)a.rows * a.q_heads;
+  const float ninf = -__builtin_inff();
+  float m = ninf, l = 0.f;
+  f2_t acc = {0.f, 0.f};
+  for (int b = 0; b < n; b += 64) {
+    const int cnt = min(64, n - b);
+    const float x = lane < cnt ? a.part_lse[(size_t)(b + lane) * stride + oi] : ninf;
+    const float mn = fmaxf(m, wave_max_f(x));
+    const float e = x == ninf ? 0.f : fast_exp2(x - mn);
+    const float alpha = m == ninf ? 0.f : fast_exp2(m - mn);
+    l = fmaf(l, alpha, wave_sum_f(e));
+    acc *= alpha;
+    m = mn;
+    for (int q = 0; q < cnt; q += 16) {
+      f2_t p[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        p[u] = f2_t{0.f, 0.f};
+        if (q + u < cnt)
+          p[u] = *reinterpret_cast<const f2_t*>(a.part_o + ((size_t)(b + q + u) * stride + oi) * kHeadDim + 2 * lane);
+      }
+#pragma unroll
+      for (int u = 0; u < 16; ++u)
+        acc += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), (q + u) & 63)) * p[u];
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  reinterpret_cast<uint32_t*>(a.out + oi * kHeadDim)[lane] = pack_bf16(acc.x * inv, acc.y * inv);
+  if (lane == 0 && a.lse) a.lse[oi] = l == 0.f ? ninf : (m + fast_log2(l)) * kLn2;
+}
+
+// Query blocks of a launch at most: a sequence's last one may not be full.
+int64_t most_blocks(const RowsArgs& a, int waves) {
+  return (int64_t)a.rows * a.group / (kRowsPerWave * waves) + a.batch;
+}
+
+template <int kWaves, int kSrc, bool kPaged>
+hipError_t launch_attn(const RowsArgs& a, hipStream_t stream) {
+  const int64_t grid = most_blocks(a, kWaves) * a.num_splits * a.kv_heads;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((k_rows_attn<kWaves, kSrc, kPaged>), dim3((uint32_t)grid), dim3(64 * kWaves), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int kSrc>
+hipError_t launch_q8(const RowsArgs& a, hipStream_t stream) {
+  const bool paged = a.c.table != nullptr;
+  hipError_t e;
+  if (rows_waves(a.batch, a.rows, a.group) == 4)
+    e = paged ? launch_attn<4, kSrc, true>(a, stream) : launch_attn<4, kSrc, false>(a, stream);
+  else
+    e = paged ? launch_attn<8, kSrc, true>(a, stream) : launch_attn<8, kSrc, false>(a, stream);
+  if (e != hipSuccess || a.num_splits == 1) return e;
+  const int64_t outs = (int64_t)a.rows * a.q_heads;
+  hipLaunchKernelGGL(k_rows_combine<kSrc>, dim3((uint32_t)((outs + 3) / 4)), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Waves of a workgroup: four (128 rows) where a sequence's rows are no more.
+int32_t rows_waves(int32_t batch, int32_t rows, int32_t group) {
+  return (int64_t)rows * group <= (int64_t)128 * batch ? 4 : 8;
+}
+
+// Key splits at most: enough for two workgroups a CU (4 waves) or one (8).
+static int64_t rows_most_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows) {
+  const int waves = rows_waves(batch, rows, group);
+  const int64_t per = kRowsPerWave * waves;
+  const int64_t each = ((int64_t)((rows + batch - 1) / batch) * group + per - 1) / per;
+  const int64_t wgs = (each < 1 ? 1 : each) * batch * kv_heads;
+  const int64_t want = waves == 4 ? 2 * kCus : kCus;
+  return wgs >= want ? 1 : (want + wgs - 1) / wgs;
+}
+
+int32_t rows_chunk(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
+  const int64_t most = rows_most_splits(batch, kv_heads, group, rows);
+  int64_t chunk = ((max_seq_len + most - 1) / most + 63) / 64 * 64;
+  return (int32_t)(chunk < 128 ? 128 : chunk);
+}
+
+// A bound on the splits that never decreases as the length grows.
+int32_t rows_max_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
+  const int64_t most = rows_most_splits(batch, kv_heads, group, rows);
+  const int64_t by_len = ((int64_t)max_seq_len + 127) / 128;
+  const int64_t s = by_len < most ? by_len : most;
+  return (int32_t)(s < 1 ? 1 : s);
+}
+
+hipError_t launch_rows_q8(const RowsArgs& a, int32_t format, hipStream_t stream) {
+  return format == RESA_Q8_INT8 ? launch_q8<RESA_Q8_INT8>(a, stream) : launch_q8<RESA_Q8_E4M3>(a, stream);
+}
+
+hipError_t launch_prompt(const RowsArgs& a, hipStream_t stream) {
+  // Small launches in 4-wave workgroups, two a CU.
+  return most_blocks(a, 8) * a.kv_heads < 2 * kCus ? launch_attn<4, kPacked, false>(a, stream)
+                                                   : launch_attn<8, kPacked, false>(a, stream);
+}
+
+}  // namespace resa
