@@ -39,6 +39,7 @@ __all__ = ["KVCache", "Workspace", "ResaError", "num_selected", "block_summarize
            "load_rows_q8", "sparse_decode_q8", "dense_rectify_q8"]
 
 HEAD_DIM = 128
+_SCALE = 1.0 / math.sqrt(HEAD_DIM)
 
 
 def _ptr(t: torch.Tensor | None) -> int | None:
@@ -477,7 +478,18 @@ class KVCacheQ8:
     def desc(self):
         raise TypeError("an 8-bit cache: use the calls that end in _q8 (and select_blocks)")
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_checked", None)
+
     def desc_q8(self) -> KVCacheQ8Desc:
+        """The library's description of this cache. Its tensors are checked once
+        and again after one was replaced or moved (checking them took 8 us a call)."""
+        where = (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                 self.kmin.data_ptr(), self.kmax.data_ptr())
+        checked = self._checked
+        if checked is not None and checked[0] == where:
+            return checked[1]
         k, b, table = self.k, self.block_size, self.block_table
         fmt = _Q8_FORMATS.get(k.dtype)
         if fmt is None:
@@ -495,14 +507,23 @@ class KVCacheQ8:
         _need(self.v_scale, "v_scale", torch.float32, scales)
         _need(self.kmin, "kmin", torch.bfloat16, (B, H, mb, HEAD_DIM))
         _need(self.kmax, "kmax", torch.bfloat16, (B, H, mb, HEAD_DIM))
-        return KVCacheQ8Desc(KVCacheDesc(k.data_ptr(), self.v.data_ptr(), self.kmin.data_ptr(), self.kmax.data_ptr(),
-                                         B, H, HEAD_DIM, mb * b, b, tp, pages),
-                             self.k_scale.data_ptr(), self.v_scale.data_ptr(), fmt)
+        _one_device(k, self.v, self.k_scale, self.v_scale, self.kmin, self.kmax, table)
+        d = KVCacheQ8Desc(KVCacheDesc(where[0], where[1], where[4], where[5], B, H, HEAD_DIM, mb * b, b, tp, pages),
+                          where[2], where[3], fmt)
+        object.__setattr__(self, "_checked", (where, d))
+        return d
 
 
 def _packed(t: torch.Tensor, name: str, rows: int, heads: int) -> int:
     """Checks packed rows ``[rows, heads, 128]`` (bf16, a row contiguous) and
     returns the elements from one row to the next."""
+    try:  # the usual case in one expression
+        row, head, dim = t.stride()
+        if t.dtype is torch.bfloat16 and t.is_cuda and t.shape == (rows, heads, HEAD_DIM) and dim == 1 \
+                and head == HEAD_DIM and not t.requires_grad:
+            return row if rows > 1 else heads * HEAD_DIM
+    except (AttributeError, TypeError, ValueError):
+        pass
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype is not torch.bfloat16:
@@ -519,19 +540,44 @@ def _packed(t: torch.Tensor, name: str, rows: int, heads: int) -> int:
     return row if rows > 1 else heads * HEAD_DIM
 
 
-def _same_device(first: torch.Tensor, *others) -> None:
-    """Every tensor of a call is on the current device, whose stream it runs on."""
-    index = first.device.index
+_devices = None
+
+
+def _one_device(first: torch.Tensor, *others) -> None:
+    """Every tensor of a call lies on the current device, whose stream it runs on."""
+    global _devices
+    if _devices is None:
+        _devices = torch.cuda.device_count()
+    if _devices == 1:  # what is on a GPU is on this one
+        return
+    index = first.get_device()
     if index != _current_device():
         raise ValueError(f"tensors are on device {index}, the current device is {_current_device()}")
     for t in others:
-        if t is not None and t.device.index != index:
-            raise ValueError(f"tensors are on devices {index} and {t.device.index}")
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"tensors are on devices {index} and {t.get_device()}")
 
 
-def _allocating(stream):
-    """What a call allocates belongs to the stream that it runs on."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+def _new(stream, device, *wanted):
+    """New tensors ((shape, dtype), ...) that belong to the stream a call runs on."""
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
+
+
+def _with_workspace(call, needs, workspace, stream, device):
+    """call(pointer, bytes) on the workspace as it is; where the library finds it
+    too small (before it enqueues anything), on one of needs() bytes."""
+    ws = workspace.buf if workspace is not None else None
+    if ws is not None:
+        rc = call(ws.data_ptr(), ws.numel())
+        if rc != _ERR_WORKSPACE:
+            return check(rc)
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        ws = (workspace or Workspace(device)).get(needs())
+    check(call(ws.data_ptr(), ws.numel()))
+
+
+_ERR_WORKSPACE = 3
 
 
 def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
@@ -548,16 +594,15 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     B = cu_seqlens.shape[0] - 1
     _need(cu_seqlens, "cu_seqlens", torch.int32, (B + 1,))
     if sm_scale is None:
-        sm_scale = 1.0 / math.sqrt(HEAD_DIM)
-    with _allocating(stream):
-        if out is None:
-            out = torch.empty((T, hq, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
-        if lse is None and with_lse:
-            lse = torch.empty((T, hq), dtype=torch.float32, device=q.device)
+        sm_scale = _SCALE
+    if out is None:
+        out, = _new(stream, q.device, ((T, hq, HEAD_DIM), torch.bfloat16))
+    if lse is None and with_lse:
+        lse, = _new(stream, q.device, ((T, hq), torch.float32))
     _need(out, "out", torch.bfloat16, (T, hq, HEAD_DIM))
     if lse is not None:
         _need(lse, "lse", torch.float32, (T, hq))
-    _same_device(q, k, v, cu_seqlens, out, lse)
+    _one_device(q, k, v, cu_seqlens, out, lse)
     if T:  # an empty tensor has no address
         check(lib().resa_prompt_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), qs, ks, vs, hq, hkv, HEAD_DIM,
                                           cu_seqlens.data_ptr(), B, T, float(sm_scale), out.data_ptr(), _ptr(lse),
@@ -572,12 +617,12 @@ def store_rows_q8(cache: KVCacheQ8, k_rows: torch.Tensor, v_rows: torch.Tensor, 
     ``[cu_rows[s], cu_rows[s + 1])`` of k_rows, v_rows ``[T, Hkv, 128]`` (bf16)
     become the last positions of sequence s, whose ``seq_lens`` already counts
     them."""
-    T = k_rows.shape[0]
-    ks, vs = _packed(k_rows, "k_rows", T, cache.kv_heads), _packed(v_rows, "v_rows", T, cache.kv_heads)
-    _need(cu_rows, "cu_rows", torch.int32, (cache.batch + 1,))
-    _need(seq_lens, "seq_lens", torch.int32, (cache.batch,))
     d = cache.desc_q8()
-    _same_device(cache.k, k_rows, v_rows, cu_rows, seq_lens)
+    B, H, T = d.base.batch, d.base.num_kv_heads, k_rows.shape[0]
+    ks, vs = _packed(k_rows, "k_rows", T, H), _packed(v_rows, "v_rows", T, H)
+    _need(cu_rows, "cu_rows", torch.int32, (B + 1,))
+    _need(seq_lens, "seq_lens", torch.int32, (B,))
+    _one_device(cache.k, k_rows, v_rows, cu_rows, seq_lens)
     if T:
         check(lib().resa_store_rows_q8(C.byref(d), k_rows.data_ptr(), v_rows.data_ptr(), ks, vs, cu_rows.data_ptr(),
                                        T, seq_lens.data_ptr(), _stream(stream)))
@@ -587,20 +632,19 @@ def load_rows_q8(cache: KVCacheQ8, cu_rows: torch.Tensor, seq_lens: torch.Tensor
                  out: tuple | None = None, stream=None):
     """The last rows of each sequence as bf16, ``(k_rows, v_rows)`` of ``[T,
     Hkv, 128]``: ``out``, or new tensors of ``num_rows`` rows."""
+    d = cache.desc_q8()
+    B, H = d.base.batch, d.base.num_kv_heads
     if out is None:
         if num_rows is None:
             raise ValueError("either num_rows or out must be given")
-        with _allocating(stream):
-            out = tuple(torch.empty((num_rows, cache.kv_heads, HEAD_DIM), dtype=torch.bfloat16,
-                                    device=cache.k.device) for _ in "kv")
+        out = tuple(_new(stream, cache.k.device, *[((num_rows, H, HEAD_DIM), torch.bfloat16)] * 2))
     k_rows, v_rows = out
     T = k_rows.shape[0]
-    _need(k_rows, "k_rows", torch.bfloat16, (T, cache.kv_heads, HEAD_DIM))
-    _need(v_rows, "v_rows", torch.bfloat16, (T, cache.kv_heads, HEAD_DIM))
-    _need(cu_rows, "cu_rows", torch.int32, (cache.batch + 1,))
-    _need(seq_lens, "seq_lens", torch.int32, (cache.batch,))
-    d = cache.desc_q8()
-    _same_device(cache.k, k_rows, v_rows, cu_rows, seq_lens)
+    _need(k_rows, "k_rows", torch.bfloat16, (T, H, HEAD_DIM))
+    _need(v_rows, "v_rows", torch.bfloat16, (T, H, HEAD_DIM))
+    _need(cu_rows, "cu_rows", torch.int32, (B + 1,))
+    _need(seq_lens, "seq_lens", torch.int32, (B,))
+    _one_device(cache.k, k_rows, v_rows, cu_rows, seq_lens)
     if T:
         check(lib().resa_load_rows_q8(C.byref(d), cu_rows.data_ptr(), T, seq_lens.data_ptr(), k_rows.data_ptr(),
                                       v_rows.data_ptr(), _stream(stream)))
@@ -613,30 +657,27 @@ def sparse_decode_q8(cache: KVCacheQ8, q: torch.Tensor, seq_lens: torch.Tensor, 
                      workspace: Workspace | None = None, stream=None):
     """:func:`sparse_decode` over an 8-bit cache. Returns ``(out fp32 [B, Hq,
     128], lse fp32 [B, Hq] or None)``."""
-    B, Hkv = cache.kmin.shape[0], cache.k.shape[1]
-    hq = q.shape[1]
+    d = cache.desc_q8()
+    B, H, hq, n_cap = d.base.batch, d.base.num_kv_heads, q.shape[1], block_idx.shape[-1]
     _need(q, "q", torch.bfloat16, (B, hq, HEAD_DIM))
     _need(seq_lens, "seq_lens", torch.int32, (B,))
-    n_cap = block_idx.shape[-1]
-    _need(block_idx, "block_idx", torch.int32, (B, Hkv, n_cap))
-    _need(num_sel, "num_sel", torch.int32, (B, Hkv))
-    if sm_scale is None:
-        sm_scale = 1.0 / math.sqrt(HEAD_DIM)
-    ws_bytes = lib().resa_decode_q8_workspace_size(B, Hkv, hq, n_cap, cache.block_size, num_splits)
-    with _allocating(stream):
-        if out is None:
-            out = torch.empty((B, hq, HEAD_DIM), dtype=torch.float32, device=q.device)
-        if lse is None and with_lse:
-            lse = torch.empty((B, hq), dtype=torch.float32, device=q.device)
-        ws = (workspace or Workspace(q.device)).get(ws_bytes)
+    _need(block_idx, "block_idx", torch.int32, (B, H, n_cap))
+    _need(num_sel, "num_sel", torch.int32, (B, H))
+    if out is None:
+        out, = _new(stream, q.device, ((B, hq, HEAD_DIM), torch.float32))
+    if lse is None and with_lse:
+        lse, = _new(stream, q.device, ((B, hq), torch.float32))
     _need(out, "out", torch.float32, (B, hq, HEAD_DIM))
     if lse is not None:
         _need(lse, "lse", torch.float32, (B, hq))
-    d = cache.desc_q8()
-    _same_device(cache.k, q, seq_lens, block_idx, num_sel, out, lse, ws)
-    check(lib().resa_sparse_decode_q8(C.byref(d), q.data_ptr(), hq, seq_lens.data_ptr(), block_idx.data_ptr(),
-                                      num_sel.data_ptr(), n_cap, num_splits, float(sm_scale), out.data_ptr(),
-                                      _ptr(lse), ws.data_ptr(), ws.numel(), _stream(stream)))
+    _one_device(cache.k, q, seq_lens, block_idx, num_sel, out, lse)
+    scale = _SCALE if sm_scale is None else float(sm_scale)
+    ptrs = (C.byref(d), q.data_ptr(), hq, seq_lens.data_ptr(), block_idx.data_ptr(), num_sel.data_ptr(), n_cap,
+            num_splits, scale, out.data_ptr(), _ptr(lse))
+    run, st = lib().resa_sparse_decode_q8, _stream(stream)
+    _with_workspace(lambda ws, size: run(*ptrs, ws, size, st),
+                    lambda: lib().resa_decode_q8_workspace_size(B, H, hq, n_cap, cache.block_size, num_splits),
+                    workspace, stream, q.device)
     return out, lse
 
 
@@ -651,29 +692,26 @@ def dense_rectify_q8(cache: KVCacheQ8, q_rows: torch.Tensor, k_rows: torch.Tenso
     ``max_seq_len`` bounds seq_lens. Returns ``(out bf16 [T, Hq, 128], lse fp32
     [T, Hq] or None)``; rows of sequences without rows in the call are not
     written."""
-    B, Hkv = cache.kmin.shape[0], cache.k.shape[1]
-    T, hq = q_rows.shape[0], q_rows.shape[1]
+    d = cache.desc_q8()
+    B, H, T, hq = d.base.batch, d.base.num_kv_heads, q_rows.shape[0], q_rows.shape[1]
     qs = _packed(q_rows, "q_rows", T, hq)
-    ks, vs = _packed(k_rows, "k_rows", T, Hkv), _packed(v_rows, "v_rows", T, Hkv)
+    ks, vs = _packed(k_rows, "k_rows", T, H), _packed(v_rows, "v_rows", T, H)
     _need(cu_rows, "cu_rows", torch.int32, (B + 1,))
     _need(seq_lens, "seq_lens", torch.int32, (B,))
-    if sm_scale is None:
-        sm_scale = 1.0 / math.sqrt(HEAD_DIM)
-    ws_bytes = lib().resa_rectify_q8_workspace_size(B, Hkv, hq, T, max_seq_len)
-    with _allocating(stream):
-        if out is None:
-            out = torch.empty((T, hq, HEAD_DIM), dtype=torch.bfloat16, device=q_rows.device)
-        if lse is None and with_lse:
-            lse = torch.empty((T, hq), dtype=torch.float32, device=q_rows.device)
-        ws = (workspace or Workspace(q_rows.device)).get(ws_bytes)
+    if out is None:
+        out, = _new(stream, q_rows.device, ((T, hq, HEAD_DIM), torch.bfloat16))
+    if lse is None and with_lse:
+        lse, = _new(stream, q_rows.device, ((T, hq), torch.float32))
     _need(out, "out", torch.bfloat16, (T, hq, HEAD_DIM))
     if lse is not None:
         _need(lse, "lse", torch.float32, (T, hq))
-    d = cache.desc_q8()
-    _same_device(cache.k, q_rows, k_rows, v_rows, cu_rows, seq_lens, out, lse, ws)
+    _one_device(cache.k, q_rows, k_rows, v_rows, cu_rows, seq_lens, out, lse)
     if T:
-        check(lib().resa_dense_rectify_q8(C.byref(d), q_rows.data_ptr(), k_rows.data_ptr(), v_rows.data_ptr(), qs, ks,
-                                          vs, hq, cu_rows.data_ptr(), T, seq_lens.data_ptr(), max_seq_len,
-                                          float(sm_scale), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(),
-                                          _stream(stream)))
+        scale = _SCALE if sm_scale is None else float(sm_scale)
+        ptrs = (C.byref(d), q_rows.data_ptr(), k_rows.data_ptr(), v_rows.data_ptr(), qs, ks, vs, hq,
+                cu_rows.data_ptr(), T, seq_lens.data_ptr(), max_seq_len, scale, out.data_ptr(), _ptr(lse))
+        run, st = lib().resa_dense_rectify_q8, _stream(stream)
+        _with_workspace(lambda ws, size: run(*ptrs, ws, size, st),
+                        lambda: lib().resa_rectify_q8_workspace_size(B, H, hq, T, max_seq_len),
+                        workspace, stream, q_rows.device)
     return out, lse

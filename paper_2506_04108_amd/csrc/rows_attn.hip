@@ -32,10 +32,16 @@
 // heads of a block next to each other: workgroups go to the 8 XCDs in turn,
 // so that with 8 kv heads the blocks of one head share an L2.
 //
-// 8-bit cache: the codes are bf16 values, so both products are on the codes
-// themselves; a block's key scale multiplies the score (inside the fma of the
-// weight) and its value scale the weight. Codes go through registers, a
-// conversion per workgroup, into the same LDS tiles.
+// 8-bit cache: every code is a bf16 and an fp16 value, so both products are on
+// the codes themselves; a block's key scale multiplies the score (inside the fma
+// of the weight) and its value scale the weight, which is fp16 here (2^-11: the
+// result's own rounding is the larger by far). The codes go from HBM into LDS,
+// a round later through registers, converted under P.V's MFMAs, into the tiles.
+// 8 x 64K, 32 rows of 4 heads each: 402 -> 370 us a call against codes and
+// scales held in registers on their way (whose copies from one register to
+// another waited for the loads), at 2.0 GHz: the chip is at its power limit
+// here too, as in long prompts (1.75 GHz, the matrix cores busy 64 % of the
+// cycles and the VALU 55 %).
 //
 // Masked keys: scores are replaced, so nothing of a masked K row matters; a
 // masked V row meets weights of zero, which only a value that is not finite
@@ -56,9 +62,11 @@ typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kRowsPerWave = 32;
-constexpr int kLoadRows = 8;               // tile rows whose K and V each wave brings in
+constexpr int kKT = 64;                    // keys per tile
+constexpr int kKT32 = kKT / 32, kKT16 = kKT / 16;
 constexpr int kRowBytes = kHeadDim * 2;
 constexpr int kCus = 256;
 constexpr float kMaxWeightSum = 4096.f;
@@ -77,10 +85,6 @@ __device__ __forceinline__ i32x4_t rsrc_words(const void* p, int bytes) {
                  (int32_t)(__builtin_amdgcn_readfirstlane((uint32_t)(u >> 32)) & 0xffffu),
                  __builtin_amdgcn_readfirstlane(bytes), kBufWord3};
 }
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const void* p, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(wave_uniform(const_cast<void*>(p)), (short)0,
-                                           __builtin_amdgcn_readfirstlane(bytes), kBufWord3);
-}
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
@@ -95,6 +99,24 @@ __device__ __forceinline__ void lds_load_rows8(uint32_t lds, uint32_t voff0, uin
       "s_add_i32 m0, %1, 1024\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved) : "s"(lds), "v"(voff0), "v"(voff1), "s"(rk) : "memory", "scc");
+}
+// 1 or 2 KB of codes likewise.
+template <int kUnits>
+__device__ __forceinline__ void lds_load_codes(uint32_t lds, uint32_t voff, i32x4_t rk) {
+  if constexpr (kUnits == 2) {
+    lds_load_rows8(lds, voff, voff + 1024, rk);
+  } else {
+    uint32_t saved;
+    __asm__ volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved) : "s"(lds), "v"(voff), "s"(rk) : "memory");
+  }
+}
+// Two fp32 values that are fp16 values, packed.
+__device__ __forceinline__ uint32_t pack_f16_exact(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
 }
 __device__ __forceinline__ void compiler_fence() { __asm__ volatile("" ::: "memory"); }
 __device__ __forceinline__ void bare_barrier() {
@@ -192,21 +214,37 @@ __device__ __forceinline__ bool find_block(const RowsArgs& a, int item, int per,
   return true;
 }
 
+// LDS of a workgroup: K and V tiles of 16-bit values, tile t in stage t %
+// kStages; for an 8-bit cache also the codes of a K and of a V tile on their way
+// (each wave's rows in turn; 80 KB with two stages, so that two workgroups fit a
+// CU), for packed rows a flag.
+template <int kStages, bool kQ8>
+struct RowsLds {
+  uint8_t k[kStages][kKT * kRowBytes];
+  uint8_t v[kStages][kKT * kRowBytes];
+  int odd;  // a masked tile holds a V value that is not finite
+};
+template <int kStages>
+struct RowsLds<kStages, true> {
+  uint8_t k[kStages][kKT * kRowBytes];
+  uint8_t v[kStages][kKT * kRowBytes];
+  uint8_t raw[2][kKT * kHeadDim];
+};
+
+// Packed rows, 8 waves: one workgroup a CU, four stages of K and V. Otherwise
+// two stages, and with 4 waves two workgroups a CU. A barrier every kBar
+// tiles, half the stages.
 template <int kWaves, int kSrc, bool kPaged>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_rows_attn(RowsArgs a) {
   constexpr bool kQ8 = kSrc != kPacked;
   // Weights and V: bf16, or over codes fp16.
   typedef std::conditional_t<kQ8, f16x8_t, bf16x8_t> P8;
-  constexpr int kKT = kLoadRows * kWaves;  // keys per tile
-  constexpr int kKT32 = kKT / 32, kKT16 = kKT / 16;
+  constexpr int kStages = kWaves == 8 && !kQ8 ? 4 : 2, kBar = kStages / 2;
+  constexpr int kLoadRows = kKT / kWaves;  // tile rows whose K and V each wave brings in
+  constexpr int kUnits = kLoadRows / 8;
   constexpr int kRowsPerWg = kRowsPerWave * kWaves;
   constexpr int kTileBytes = kKT * kRowBytes;
-  struct Lds {
-    uint8_t k[4][kTileBytes];    // tile t in stage t % 4
-    uint8_t v[4][kTileBytes];
-    float fk[4][4], fv[4][4];    // 8-bit cache: factors of each 16 keys (scores, weights)
-    int odd;                     // a masked tile holds a V value that is not finite
-  };
+  typedef RowsLds<kStages, kQ8> Lds;
   __shared__ __attribute__((aligned(1024))) Lds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hk = blockIdx.x % a.kv_heads;
@@ -237,17 +275,19 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const int cut = min(k1, past + min(row_base, R - 1) / G);
   const int wg_cut = past + qblk * kRowsPerWg / G;
 
-  // Packed rows straight into LDS: lane i fills slot i % 16 of rows wrow +
-  // i / 16 and + 4, fetching the row's piece (i % 16) ^ swz(row).
+  // Packed rows straight into LDS: lane i fills slot i % 16 of rows i / 16 and
+  // + 4 of each eight, fetching the row's piece (i % 16) ^ swz(row).
   const int wrow = kLoadRows * wave;
   const int lrow = lane >> 4, lslot = lane & 15;
-  uint32_t koff[2], voff[2];
+  uint32_t koff[kUnits][2], voff[kUnits][2];
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const uint32_t piece = 16 * (lslot ^ swz(wrow + 4 * e + lrow));
-    koff[e] = (uint32_t)(4 * e + lrow) * (uint32_t)(2 * a.k_stride) + piece;
-    voff[e] = (uint32_t)(4 * e + lrow) * (uint32_t)(2 * a.v_stride) + piece;
-  }
+  for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t piece = 16 * (lslot ^ swz(wrow + 8 * u + 4 * e + lrow));
+      koff[u][e] = (uint32_t)(8 * u + 4 * e + lrow) * (uint32_t)(2 * a.k_stride) + piece;
+      voff[u][e] = (uint32_t)(8 * u + 4 * e + lrow) * (uint32_t)(2 * a.v_stride) + piece;
+    }
   const uint32_t lds0 = lds_addr(&lds);
   const uint32_t lds_k = __builtin_amdgcn_readfirstlane(lds0) + (uint32_t)(wrow * kRowBytes);
   // LDS read addresses (stage, 32-key part and k-step of P.V are immediates).
@@ -255,7 +295,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   // 16 passing the address of key c / 4, dims 4 (c % 4) .. ; eight rows further
   // the slots differ in bit 1. The pieces of k-step ks and of dims 32 dt are an
   // exclusive or with 32 ks and 64 dt, taken once a round: held in registers
-  // they made the 8-wave kernels spill.
+  // they make the kernels spill.
   uint32_t kbase = lds0 + lq * kRowBytes + 16 * (hi ^ swz(lq));
   uint32_t vbase;
   {
@@ -266,6 +306,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   auto fresh = [](uint32_t& x) __attribute__((always_inline)) { __asm__ volatile("" : "+v"(x)); };
   typedef __attribute__((address_space(3))) const bf16x8_t lds_bf16x8;
   typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
+  typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4;
   auto read_k = [&](int st, int ks, bf16x8_t (&ka)[kKT32]) __attribute__((always_inline)) {
 #pragma unroll
     for (int kt = 0; kt < kKT32; ++kt)
@@ -303,12 +344,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     return min(max(k1 - (k0 + ti * kKT + wrow), 0), kLoadRows);
   };
   // Packed keys: K and V of a tile, requested straight into their stages.
-  auto issue_packed = [&](const uint16_t* p, int64_t stride, const uint32_t (&off)[2], uint32_t to, int ti)
+  auto issue_packed = [&](const uint16_t* p, int64_t stride, const uint32_t (&off)[kUnits][2], uint32_t to, int ti)
                           __attribute__((always_inline)) {
     const int have = rows_of(ti);
     const int nrec = have > 0 ? (have - 1) * (int)(2 * stride) + kRowBytes : 0;
-    lds_load_rows8(to, off[0], off[1],
-                   rsrc_words(p + (int64_t)(sr.first + k0 + ti * kKT + wrow) * stride + hk * kHeadDim, nrec));
+    const i32x4_t rx = rsrc_words(p + (int64_t)(sr.first + k0 + ti * kKT + wrow) * stride + hk * kHeadDim, nrec);
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) lds_load_rows8(to + 8 * u * kRowBytes, off[u][0], off[u][1], rx);
   };
   auto issue_k = [&](int ti, int st) __attribute__((always_inline)) {
     issue_packed(a.k, a.k_stride, koff, lds_k + (uint32_t)(st * kTileBytes), ti);
@@ -316,78 +358,142 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   auto issue_v = [&](int ti, int st) __attribute__((always_inline)) {
     issue_packed(a.v, a.v_stride, voff, lds_k + (uint32_t)(offsetof(Lds, v) + st * kTileBytes), ti);
   };
-  // 8-bit cache: the wave's eight rows of a tile (they lie in one block) are
-  // 1 KB, 16 codes of row lane / 8 a lane, held until they are converted.
-  struct Codes {
-    U4 x;
-    float ks, vs;
+  // 8-bit cache. Lane i holds the page and the factors of block i of a window
+  // of 64 blocks, which a wave takes with a lane read, with no load in the way;
+  // the window moves by 32 blocks, the one after it on its way: the tile at hand
+  // lies in its first half, and the (at most 16) blocks of the next three
+  // tiles in it too. A block with a scale that is no finite number (it was made
+  // of rows that held one) is `odd`: it has NaN for its keys, so whoever sees
+  // it gets NaN, and for the others its V counts as zero.
+  const int mb0 = kQ8 ? k0 >> a.c.log2_block : 0, mlast = kQ8 ? (k1 - 1) >> a.c.log2_block : 0;
+  struct Window {
+    int page;
+    float kf, vf;
   };
-  auto ask = [&](bool key, int ti) __attribute__((always_inline)) -> Codes {
-    Codes w;
-    const int at = k0 + ti * kKT + wrow;
-    int have = rows_of(ti);
-    const int m = min(at >> a.c.log2_block, a.c.max_blocks - 1);
-    int64_t row, si;
+  Window win, coming;
+  int wbase = 0;      // the window's first block, from mb0 on
+  uint64_t odd = 0;   // its odd blocks
+  auto load_window = [&](int base) __attribute__((always_inline)) -> Window {
+    Window w;
+    const int m = min(mb0 + base + lane, mlast);
+    int64_t si;
+    w.page = 0;
     if constexpr (kPaged) {
-      const int page = __builtin_amdgcn_readfirstlane(a.c.table[(size_t)seq * a.c.max_blocks + m]);
-      if ((unsigned)page >= (unsigned)a.c.num_pages) have = 0;
-      const int64_t p = have > 0 ? page : 0;
-      si = p * a.c.kv_heads + hk;
-      row = si * a.c.block_size + (at & (a.c.block_size - 1));
+      w.page = a.c.table[(size_t)seq * a.c.max_blocks + m];
+      if ((unsigned)w.page >= (unsigned)a.c.num_pages) w.page = -1;
+      si = (int64_t)max(w.page, 0) * a.kv_heads + hk;
     } else {
-      const int64_t grp = (int64_t)seq * a.c.kv_heads + hk;
-      si = grp * a.c.max_blocks + m;
-      row = grp * a.c.capacity + at;
+      si = ((int64_t)seq * a.kv_heads + hk) * a.c.max_blocks + m;
     }
-    const uint8_t* base = reinterpret_cast<const uint8_t*>(key ? a.c.k : a.c.v);
-    const __amdgpu_buffer_rsrc_t rx = uniform_rsrc(base + row * kHeadDim, have * kHeadDim);
-    w.x = __builtin_bit_cast(U4, __builtin_amdgcn_raw_buffer_load_b128(rx, 16 * lane, 0, 0));
-    const __amdgpu_buffer_rsrc_t rv = uniform_rsrc(a.v_scale + si, 4);
-    w.vs = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rv, 0, 0, 0));
-    w.ks = 0.f;
-    if (key) {
-      const __amdgpu_buffer_rsrc_t rk = uniform_rsrc(a.k_scale + si, 4);
-      w.ks = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rk, 0, 0, 0));
-    }
+    w.kf = a.k_scale[si];
+    w.vf = a.v_scale[si];
     return w;
   };
-  // Converted into the tile's stage. A block with a scale that is no finite
-  // number (it was made of rows that held one) has NaN for its keys: whoever
-  // sees it gets NaN, and for the others its V counts as zero.
-  auto put = [&](bool key, const Codes& w, int st) __attribute__((always_inline)) {
+  auto take_window = [&](const Window& w) __attribute__((always_inline)) {
+    const bool bad = !finite_f(w.kf) || !finite_f(w.vf);
+    odd = __ballot(bad);
+    win.page = w.page;
+    win.kf = bad ? c : w.kf * c;
+    win.vf = bad ? 0.f : w.vf;
+  };
+  // Block of key k0 + key (key a multiple of 16) in the window.
+  auto block_at = [&](int key) __attribute__((always_inline)) -> int { return (key >> a.c.log2_block) - wbase; };
+  auto lane_f = [&](float x, int i) __attribute__((always_inline)) -> float {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i));
+  };
+  // The wave's codes of a tile (its rows lie in one block; 1 or 2 KB, 16 codes
+  // of row lane / 8 (and + 8) a lane) into LDS at `to`.
+  auto ask = [&](bool key, int ti, uint32_t to) __attribute__((always_inline)) {
     if constexpr (kQ8) {
-      const bool odd = !finite_f(w.vs) || (key && !finite_f(w.ks));
-      uint32_t h[8];
-      const uint32_t in[4] = {w.x.x, w.x.y, w.x.z, w.x.w};
+      const int at = k0 + ti * kKT + wrow;
+      int have = rows_of(ti);
+      int64_t row;
+      if constexpr (kPaged) {
+        const int page = __builtin_amdgcn_readlane(win.page, block_at(ti * kKT + (wrow & ~15)));
+        if (page < 0) have = 0;
+        row = ((int64_t)max(page, 0) * a.kv_heads + hk) * a.c.block_size + (at & (a.c.block_size - 1));
+      } else {
+        row = ((int64_t)seq * a.kv_heads + hk) * a.c.capacity + at;
+      }
+      lds_load_codes<kUnits>(to, 16 * lane, rsrc_words(reinterpret_cast<const uint8_t*>(key ? a.c.k : a.c.v) +
+                                                       row * kHeadDim, have * kHeadDim));
+    }
+  };
+  const uint32_t raw_of_wave = (uint32_t)(wave * kUnits * 1024);
+  auto raw_at = [&](bool key) __attribute__((always_inline)) -> uint32_t {
+    if constexpr (kQ8)
+      return __builtin_amdgcn_readfirstlane(lds0) + (uint32_t)offsetof(Lds, raw) + (key ? 0 : kKT * kHeadDim) + raw_of_wave;
+    else
+      return 0;
+  };
+  // Where this lane's codes go in a tile: pieces 2 (lane % 8) and + 1 of row
+  // wrow + lane / 8 (and of row + 8, where slots differ in bit 1).
+  const int put_row = wrow + (lane >> 3);
+  const uint32_t put0 = put_row * kRowBytes + 16 * ((2 * (lane & 7)) ^ swz(put_row));
+  const uint32_t put1 = put_row * kRowBytes + 16 * ((2 * (lane & 7) + 1) ^ swz(put_row));
+  // Four codes as 16-bit values: of a key bf16, of a value fp16.
+  auto convert = [&](bool key, uint32_t in, uint32_t (&h)[2]) __attribute__((always_inline)) {
+    if constexpr (kSrc == RESA_Q8_INT8) {
+      float y[4];
+      codes_f32<kSrc>(in, y);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (kSrc == RESA_Q8_INT8) {
-          float y[4];
-          codes_f32<kSrc>(in[i], y);
+      for (int u = 0; u < 2; ++u)
+        h[u] = key ? __builtin_amdgcn_perm(__float_as_uint(y[2 * u + 1]), __float_as_uint(y[2 * u]), 0x07060302u)
+                   : pack_f16_exact(y[2 * u], y[2 * u + 1]);
+    } else if (key) {
+      h[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in, 1.f, false));
+      h[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in, 1.f, true));
+    } else {
+      h[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in, 1.f, false));
+      h[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in, 1.f, true));
+    }
+  };
+  // The codes of this wave's rows of a tile, arrived in LDS at `from`.
+  struct Codes {
+    u32x4_t x[kUnits];
+  };
+  auto codes_at = [&](uint32_t from) __attribute__((always_inline)) -> Codes {
+    Codes w;
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
-            h[2 * i + u] = key ? __builtin_amdgcn_perm(__float_as_uint(y[2 * u + 1]), __float_as_uint(y[2 * u]), 0x07060302u)
-                               : __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)y[2 * u], (_Float16)y[2 * u + 1]});
-        } else if (key) {
-          h[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in[i], 1.f, false));
-          h[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(in[i], 1.f, true));
-        } else {
-          h[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[i], 1.f, false));
-          h[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[i], 1.f, true));
+    for (int q = 0; q < kUnits; ++q) w.x[q] = *(lds_u32x4*)(uintptr_t)(from + 16 * lane + 1024 * q);
+    return w;
+  };
+  // Word w (0 .. 4 kUnits - 1) of them converted; every second one stores eight
+  // values to stage st (half: the four before).
+  auto put_word = [&](bool key, const Codes& c8, int w, int st, uint32_t (&half)[2]) __attribute__((always_inline)) {
+    uint32_t h[2];
+    convert(key, c8.x[w / 4][w % 4], h);
+    if (w % 2 == 0) {
+      half[0] = h[0];
+      half[1] = h[1];
+    } else {
+      uint8_t* tile = key ? lds.k[st] : lds.v[st];
+      st16(tile + 8 * (w / 4) * kRowBytes + ((w % 4 == 1 ? put0 : put1) ^ (32 * (w / 4))), U4{half[0], half[1], h[0], h[1]});
+    }
+  };
+  // Rows of tile ti of an odd block: NaN keys, zero values.
+  auto put_odd = [&](bool key, int ti, int st) __attribute__((always_inline)) {
+    if constexpr (kQ8) {
+      if (__builtin_expect((odd >> block_at(ti * kKT + (wrow & ~15))) & 1, 0)) {
+        uint8_t* tile = key ? lds.k[st] : lds.v[st];
+        const uint32_t x = key ? 0x7fc07fc0u : 0u;
+#pragma unroll
+        for (int q = 0; q < kUnits; ++q) {
+          st16(tile + 8 * q * kRowBytes + (put0 ^ (32 * q)), U4{x, x, x, x});
+          st16(tile + 8 * q * kRowBytes + (put1 ^ (32 * q)), U4{x, x, x, x});
         }
       }
-      if (__builtin_expect(__any(odd), 0)) {
+    }
+  };
+  auto put = [&](bool key, int ti, uint32_t from, int st) __attribute__((always_inline)) {
+    if constexpr (kQ8) {
+      compiler_fence();
+      const Codes w = codes_at(from);
+      uint32_t half[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = key ? 0x7fc07fc0u : 0u;
-      }
-      const int row = wrow + (lane >> 3), piece = 2 * (lane & 7);
-      uint8_t* tile = key ? lds.k[st] : lds.v[st];
-      st16(tile + row * kRowBytes + 16 * (piece ^ swz(row)), U4{h[0], h[1], h[2], h[3]});
-      st16(tile + row * kRowBytes + 16 * ((piece + 1) ^ swz(row)), U4{h[4], h[5], h[6], h[7]});
-      if ((wave & 1) == 0 && lane == 0) {
-        if (key) lds.fk[st][wave >> 1] = odd ? c : w.ks * c;
-        else lds.fv[st][wave >> 1] = odd ? 0.f : w.vs;
-      }
+      for (int i = 0; i < 4 * kUnits; ++i) put_word(key, w, i, st, half);
+      put_odd(key, ti, st);
+      compiler_fence();  // the codes have been read when the next are asked for
     }
   };
 
@@ -414,34 +520,34 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   struct Factors {
     float x[kKT16];
   };
-  auto key_factors = [&](int st) __attribute__((always_inline)) -> Factors {
+  auto key_factors = [&](int ti) __attribute__((always_inline)) -> Factors {
     Factors f;
 #pragma unroll
-    for (int i = 0; i < kKT16; ++i) f.x[i] = kQ8 ? lds.fk[st][i] : c;
+    for (int i = 0; i < kKT16; ++i) f.x[i] = kQ8 ? lane_f(win.kf, block_at(ti * kKT + 16 * i)) : c;
     return f;
   };
   // fp16 weights carry the value scale over vref, a power of two above the
   // largest value scale met so far, which the accumulators are in units of.
-  float vref = 0x1p-126f;
-  auto value_factors = [&](int st) __attribute__((always_inline)) -> Factors {
+  uint32_t vref = 0x00800000u;  // bits of 2^-126
+  auto value_factors = [&](int ti) __attribute__((always_inline)) -> Factors {
     Factors f;
     if constexpr (kQ8) {
-      float top = 0.f;
+      uint32_t x[kKT16], top = 0;
 #pragma unroll
       for (int i = 0; i < kKT16; ++i) {
-        f.x[i] = lds.fv[st][i];
-        top = fmaxf(top, f.x[i]);
+        x[i] = __float_as_uint(lane_f(win.vf, block_at(ti * kKT + 16 * i)));
+        top = max(top, x[i]);  // of bit patterns: scales are not negative
       }
-      if (__builtin_expect(__any(top > vref), 0)) {
-        const float up = __uint_as_float((__float_as_uint(top) & 0x7f800000u) + 0x00800000u);
-        const float alpha = vref / up;
+      if (__builtin_expect(top > vref, 0)) {
+        const uint32_t up = (top & 0x7f800000u) + 0x00800000u;
+        const float alpha = __uint_as_float(vref) / __uint_as_float(up);
         vref = up;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
       }
-      const float inv = 1.f / vref;
+      const float inv = __uint_as_float(0x7f000000u - vref);  // 1 / vref
 #pragma unroll
-      for (int i = 0; i < kKT16; ++i) f.x[i] *= inv;
+      for (int i = 0; i < kKT16; ++i) f.x[i] = __uint_as_float(x[i]) * inv;
     }
     return f;
   };
@@ -455,7 +561,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   };
   auto weight = [&](float y, int i, const Factors& g, P8 (&ph)[kKT16], float (&ps)[4]) __attribute__((always_inline)) {
     const float pe = fast_exp2(y);
-    ps[i & 3] += pe;
+    ps[i & 3] = i < 4 ? pe : ps[i & 3] + pe;
     if constexpr (kQ8)
       ph[i >> 3][i & 7] = (_Float16)(pe * g.x[i >> 3]);
     else
@@ -492,44 +598,40 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int ks = 0; ks < 8; ++ks) {
       if (ks < 7) read_k(st, ks + 1, ka[(ks + 1) & 1]);
 #pragma unroll
-      for (int kt = 0; kt < kKT32; ++kt) sn[kt] = mfma32(ka[ks & 1][kt], qb[ks], sn[kt]);
+      for (int kt = 0; kt < kKT32; ++kt) {
+        sn[kt] = mfma32(ka[ks & 1][kt], qb[ks], sn[kt]);
 #pragma unroll
-      for (int i = 2 * kKT32 * ks; i < 2 * kKT32 * (ks + 1); ++i) weight(fmaf(s[i >> 4][i & 15], f.x[i >> 3], -m), i, g, ph, ps);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int i = 2 * (kKT32 * ks + kt); i < 2 * (kKT32 * ks + kt) + 2; ++i)
+          weight(fmaf(s[i >> 4][i & 15], f.x[i >> 3], -m), i, g, ph, ps);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     __builtin_amdgcn_s_setprio(0);
     return (ps[0] + ps[1]) + (ps[2] + ps[3]);
   };
-  Codes held[2];
   // One tile: its weights (scores s) with the next tile's scores (sn), then
   // its P.V.
   //
-  // Order between the waves, with a barrier before every even tile 2p only.
-  // Rounds 2p and 2p + 1 read K(2p + 1), K(2p + 2), V(2p) and V(2p + 1). After
-  // the barrier the stages of K(2p - 1), K(2p), V(2p - 2) and V(2p - 1) are
-  // free (last read in rounds 2p - 2 and 2p - 1); K(2p + 3), K(2p + 4),
-  // V(2p + 2) and V(2p + 3) are requested into them, and are there at the next
-  // barrier, before which every wave has waited for its own.
+  // Order between the waves, with a barrier before every kBar-th tile p only.
+  // Rounds p .. p + kBar - 1 read K(p + 1) .. K(p + kBar) and V(p) .. V(p + kBar
+  // - 1). After the barrier the stages of as many tiles before these are free;
+  // K(p + kBar + 1) .. K(p + 2 kBar) and V(p + kBar) .. V(p + 2 kBar - 1) are
+  // brought into them, and are there at the next barrier, before which every
+  // wave has waited for its own.
   auto round = [&](int ti, auto stage, f32x16_t (&s)[kKT32], f32x16_t (&sn)[kKT32], const Factors& f,
                    Factors& fn) __attribute__((always_inline)) {
     constexpr int st = decltype(stage)::value;
     const int t0 = k0 + ti * kKT;
-    if constexpr (st % 2 == 0) {
-      __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    if constexpr (st % kBar == 0) {
+      if constexpr (!kQ8) __builtin_amdgcn_s_waitcnt(kWaitVm0);
       __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
       bare_barrier();
       if constexpr (!kQ8) {
-        issue_k(ti + 3, (st + 3) & 3);
-        issue_k(ti + 4, st);
-        issue_v(ti + 2, (st + 2) & 3);
-        issue_v(ti + 3, (st + 3) & 3);
+#pragma unroll
+        for (int j = 0; j < kBar; ++j) issue_k(ti + kBar + 1 + j, (st + kBar + 1 + j) % kStages);
+#pragma unroll
+        for (int j = 0; j < kBar; ++j) issue_v(ti + kBar + j, (st + kBar + j) % kStages);
       }
-    }
-    // Codes: the two K tiles in the even round, the two V tiles in the odd.
-    if constexpr (kQ8) {
-      constexpr int ahead = st % 2 == 0 ? 3 : 1;
-      held[0] = ask(st % 2 == 0, ti + ahead);
-      held[1] = ask(st % 2 == 0, ti + ahead + 1);
     }
     if constexpr (!kQ8) {
       // What this wave brought of a tile that some row masks: any value that
@@ -537,7 +639,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       if (__builtin_expect(guard || t0 + kKT > wg_cut, 0)) {
         bool odd = false;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < 2 * kUnits; ++e) {
           uint8_t* at = lds.v[st] + (wrow + 4 * e) * kRowBytes + 16 * lane;
           const U4 x = ld16(at);
           const bool some = not_finite2(x.x) || not_finite2(x.y) || not_finite2(x.z) || not_finite2(x.w);
@@ -551,12 +653,19 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         }
       }
     }
-    const Factors g = value_factors(st);
-    fn = key_factors((st + 1) & 3);
+    if constexpr (kQ8) {
+      if (__builtin_expect(block_at(ti * kKT) >= 32, 0)) {
+        wbase += 32;
+        take_window(coming);
+        coming = load_window(wbase + 32);
+      }
+    }
+    const Factors g = value_factors(ti);
+    fn = key_factors(ti + 1);
     P8 ph[kKT16];
     fresh(kbase);
     __builtin_amdgcn_sched_barrier(0);
-    float ps = weights_scores(std::integral_constant<int, (st + 1) & 3>{}, s, sn, f, g, ph);
+    float ps = weights_scores(std::integral_constant<int, (st + 1) % kStages>{}, s, sn, f, g, ph);
     // Rare: move the reference and form the weights again. A row without one
     // so far (no tile with a finite score) takes this branch too.
     if (__builtin_expect(__any(!(ps <= kMaxWeightSum)), 0)) {
@@ -576,8 +685,17 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
     l += ps;
     if (__builtin_expect(t0 + 2 * kKT > cut, 0)) mask(t0 + kKT, sn);
+    // The codes of K(ti + 2) and V(ti + 1), asked for a round ago.
+    Codes wk, wv;
+    if constexpr (kQ8) {
+      __builtin_amdgcn_s_waitcnt(kWaitVm0);
+      compiler_fence();
+      wk = codes_at(raw_at(true));
+      wv = codes_at(raw_at(false));
+    }
     __builtin_amdgcn_sched_barrier(0);
     P8 va[2][4];
+    uint32_t half[2];
     fresh(vbase);
     read_v(st, 0, va[0]);
     __builtin_amdgcn_sched_barrier(0);
@@ -585,32 +703,55 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int ks = 0; ks < kKT16; ++ks) {
       if (ks < kKT16 - 1) read_v(st, ks + 1, va[(ks + 1) & 1]);
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt) o[dt] = mfma32(va[ks & 1][dt], ph[ks], o[dt]);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int dt = 0; dt < 4; ++dt) {
+        o[dt] = mfma32(va[ks & 1][dt], ph[ks], o[dt]);
+        // A word of codes under every MFMA (8 waves: under every second).
+        if constexpr (kQ8) {
+          const int n = 4 * ks + dt, w = n * kUnits / 2;
+          if (kUnits == 2 || n % 2 == 1) {
+            if (w < 4 * kUnits) put_word(true, wk, w, st, half);
+            else put_word(false, wv, w - 4 * kUnits, (st + 1) % kStages, half);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     if constexpr (kQ8) {
-      constexpr int ahead = st % 2 == 0 ? 3 : 1;
-      put(st % 2 == 0, held[0], (st + ahead) & 3);
-      put(st % 2 == 0, held[1], (st + ahead + 1) & 3);
+      put_odd(true, ti + 2, st);
+      put_odd(false, ti + 1, (st + 1) % kStages);
+      compiler_fence();  // the codes have been read when the next are asked for
+      ask(true, ti + 3, raw_at(true));
+      ask(false, ti + 2, raw_at(false));
     }
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  if (tid == 0) lds.odd = 0;
+  if constexpr (kQ8) {
+    take_window(load_window(0));
+    coming = load_window(32);
+  } else if (tid == 0) {
+    lds.odd = 0;
+  }
   for (;;) {
     if constexpr (kQ8) {
-      const Codes first[5] = {ask(true, 0), ask(true, 1), ask(true, 2), ask(false, 0), ask(false, 1)};
-#pragma unroll
-      for (int t = 0; t < 3; ++t) put(true, first[t], t);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) put(false, first[3 + t], t);
+      // K(1) by way of the stage that V(1) has not been put into yet.
+      const uint32_t spare = __builtin_amdgcn_readfirstlane(lds0) + (uint32_t)offsetof(Lds, v[1]) + raw_of_wave;
+      ask(true, 0, raw_at(true));
+      ask(false, 0, raw_at(false));
+      ask(true, 1, spare);
+      __builtin_amdgcn_s_waitcnt(kWaitVm0);
+      put(true, 0, raw_at(true), 0);
+      put(false, 0, raw_at(false), 0);
+      put(true, 1, spare, 1);
+      ask(true, 2, raw_at(true));
+      ask(false, 1, raw_at(false));
     } else {
 #pragma unroll
-      for (int t = 0; t < 3; ++t) issue_k(t, t);
+      for (int t = 0; t <= kBar; ++t) issue_k(t, t);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) issue_v(t, t);
+      for (int t = 0; t < kBar; ++t) issue_v(t, t);
+      __builtin_amdgcn_s_waitcnt(kWaitVm0);
     }
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     bare_barrier();
     f32x16_t sa[kKT32], sb[kKT32];
@@ -618,20 +759,26 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     if (k0 + kKT > cut) mask(k0, sa);
     Factors fa = key_factors(0), fb;
     m = row_max(sa, fa);
-    for (int ti = 0; ti < ntiles; ti += 4) {
+    for (int ti = 0; ti < ntiles; ti += kStages) {
       round(ti, std::integral_constant<int, 0>{}, sa, sb, fa, fb);
       if (ti + 1 >= ntiles) break;
       round(ti + 1, std::integral_constant<int, 1>{}, sb, sa, fb, fa);
-      if (ti + 2 >= ntiles) break;
-      round(ti + 2, std::integral_constant<int, 2>{}, sa, sb, fa, fb);
-      if (ti + 3 >= ntiles) break;
-      round(ti + 3, std::integral_constant<int, 3>{}, sb, sa, fb, fa);
+      if constexpr (kStages == 4) {
+        if (ti + 2 >= ntiles) break;
+        round(ti + 2, std::integral_constant<int, 2>{}, sa, sb, fa, fb);
+        if (ti + 3 >= ntiles) break;
+        round(ti + 3, std::integral_constant<int, 3>{}, sb, sa, fb, fa);
+      }
     }
     // No load may still be writing LDS when the workgroup ends or starts over.
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     bare_barrier();
-    if (kQ8 || guard || __builtin_expect(lds.odd == 0, 1)) break;
+    if constexpr (kQ8) {
+      break;
+    } else if (guard || __builtin_expect(lds.odd == 0, 1)) {
+      break;
+    }
     guard = true;
     clear_o();
     l = 0.f;
@@ -667,7 +814,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   }
 
   const float lt = sum_xor32(l);
-  const float inv = lt == 0.f ? 0.f : (kQ8 ? vref : 1.f) / lt;
+  const float inv = lt == 0.f ? 0.f : (kQ8 ? __uint_as_float(vref) : 1.f) / lt;
   if (rho >= R) return;
   const int row = sr.first + rho / G, head = hk * G + rho % G;
   const size_t oi = (size_t)row * a.q_heads + head;

@@ -157,6 +157,8 @@ def test_binding_refuses_before_the_device():
     c = R.KVCacheQ8.empty(1, 2, 64, 16, device="cpu")
     with pytest.raises(ValueError, match="on the GPU"):
         R.store_rows_q8(c, x, x, cu, cu[:1])
+    with pytest.raises(ValueError, match="on the GPU"):
+        c.desc_q8()
     with pytest.raises(TypeError, match="8-bit"):
         c.desc()
     c.k = c.k.view(torch.uint8)
