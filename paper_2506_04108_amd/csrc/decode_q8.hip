@@ -7,34 +7,42 @@
 // two halves in a row make a chunk of 32 tokens, the unit that is dealt to the
 // splits and their waves. Converting the codes and multiplying them on the
 // VALU would cost a multiply-add per code and query head (8 heads: 80 a clock
-// and CU at 6 TB/s, more than a CU has), so both products are MFMAs, whose
-// operands are bf16: every code (int8, e4m3) is a bf16 value.
+// and CU at 6 TB/s, more than a CU has), so both products are MFMAs.
 //
-// Lane (r, c), r = lane / 16, c = lane % 16. Per chunk:
+// Codes go from HBM into a chunk's place a wave in LDS (8 KB, whole kilobytes a
+// load and no registers); a wave reads what it needs of a chunk in the layouts of
+// the MFMAs, and the next chunk is on its way while it works on this one. Lane
+// (r, c), r = lane / 16, c = lane % 16. Per chunk:
 //   S^T = K . Q^T   two halves x four v_mfma_f32_16x16x32_bf16 (tokens x
-//                   heads). Lane (r, c) holds 32 bytes of token c: dims
-//                   16 r .. + 16 and 64 + 16 r .. + 16 (two 16-byte loads, each
-//                   wave-wide load covers 64 bytes of 16 rows); the
-//                   contraction runs over the dims in that order, and Q's rows
-//                   are held in the same. Lane (r, c) receives the scores of
-//                   head c % 8 for tokens 4 r .. + 4 of each half.
-//   weights         2^(S ks - m) in fp32, ks the block's key scale times the
-//                   softmax scale; times the block's value scale
-//   O^T += V^T . P  eight times two v_mfma_f32_16x16x32_bf16 (dims x heads):
-//                   the tokens of lane (r, c) are the ones whose weights it
-//                   holds, so P needs no exchange between lanes; V rows are
-//                   read as 8 bytes a lane (dims 8 c .. + 8 of eight tokens)
-//                   and transposed inside the lane, by the choice of the two
-//                   values that a packing instruction takes.
-// Precision: a weight (fp32) is the exact sum of three bf16 terms (8
-// significant bits each). Columns 0 .. 7 of P hold the first terms of the 8
-// heads and columns 8 .. 15 the second, so a group of up to 8 heads fills the
-// 16 columns, and a second MFMA takes the third terms; products are exact and
-// sums fp32. So the result is as exact as with fp32 arithmetic throughout, for
-// any range of the scales (they multiply the weight before it is split).
+//                   columns): lane (r, c) takes dims 16 r .. + 16 and 64 + 16 r
+//                   .. + 16 of token c; the contraction runs over the dims in
+//                   that order. Column c is head c % 8: a group has at most 8
+//                   heads, and each is there twice. Lane (r, c) receives tokens
+//                   4 r .. + 4 of each half.
+//   weights         p = 2^(S ks - m) in fp32, ks the block's key scale times the
+//                   softmax scale; w = p vs, vs the block's value scale
+//   O^T += V^T . w  eight v_mfma_f32_16x16x32_f16 (dims x columns): the tokens of
+//                   lane (r, c) are the ones whose weights it holds, so nothing
+//                   moves between lanes; it takes dims 8 c .. + 8 of them and
+//                   transposes inside the lane, by the choice of the values
+//                   that a packing instruction takes.
+// Every code is a bf16 and an fp16 value. w is the sum of two fp16 terms (22
+// bits, down to 2^-36 of the largest w met), columns 0 .. 7 holding the first
+// terms of the 8 heads and columns 8 .. 15 the second; products are exact and
+// sums fp32, so results have fp32's precision. The unit 2^-k of w belongs to a
+// head: one that sees small values alone keeps their precision whatever the
+// others see. It and the softmax reference move rarely (only then are the
+// accumulators touched).
 //
-// Bound by HBM (256 B a token and kv head); MFMA and VALU take about a third of
-// the time that the codes take to arrive.
+// Bound by HBM (256 B a token and kv head) and, with few chunks a wave, by the
+// latency of a launch, the ids, the first codes and the merge. 64K batch 8 (108
+// MB), 256K batch 1 (27 MB), 50K batch 6 paged (40 MB), 4K batch 1: 25.1, 13.7,
+// 17.6, 8.9 us (HBM at a large copy's rate: 21, 5.3, 7.8, 0.4; with codes
+// through registers, the loads in the MFMAs' layouts: 29.3, 15.6, 23.4, 9.0).
+// More chunks on their way are slower (two: 26.0, 13.8, 18.0 us, three: 27.5, 15.5,
+// 24.6), as in the bf16 decode, and so are 8 waves (25.6, 14.5, 16.9 us, 4K
+// 10.0). Both products on int8 digits, with no code converted and half of the
+// VALU work, but a longer code for every launch to fetch: 64K 34.4 against 29.3.
 #include "decode_impl.h"
 #include "rows_device.h"
 
@@ -42,30 +50,44 @@ namespace resa {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kDecodeWaves = 4;
-// Chunks in flight per wave while one is consumed.
-constexpr int kDecodeDepth = 1;
+// Chunks of a wave in LDS or on their way there, beside the one in registers.
+constexpr int kRing = 1;
+constexpr int kHalfBytes = 16 * kHeadDim;    // codes of 16 tokens
+constexpr int kChunkBytes = 4 * kHalfBytes;  // K of two halves, V of two halves
+constexpr int kChunkLoads = 8;               // loads of 1 KB
 
+// Chunk lists are staged for this many halves at a time.
+constexpr int kListed = 512;
+
+// The ring's memory serves the merges at the end.
 template <int G, int NW>
 struct DecodeQ8Lds {
-  __attribute__((aligned(16))) float racc[NW][G][kHeadDim];
-  float rm[G][NW], rl[G][NW];
-  __attribute__((aligned(16))) float own_o[G * kHeadDim];
-  float own_l[G];
-  int tok[kIdxBatch];   // first token of each half, -1: none
-  int row[kIdxBatch];
-  __attribute__((aligned(16))) float w[kMaxSplits * G];
-  f4_t red[64 * NW];
-  uint32_t ticket;
+  union {
+    __attribute__((aligned(1024))) uint8_t ring[NW][kRing][kChunkBytes];
+    struct {
+      __attribute__((aligned(16))) float racc[NW][G][kHeadDim];
+      __attribute__((aligned(16))) float own_o[G * kHeadDim];
+      __attribute__((aligned(16))) float w[kMaxSplits * G];
+      f4_t red[64 * NW];
+      float rm[G][NW], rl[G][NW];
+      float own_l[G];
+      uint32_t ticket;
+    };
+  };
+  int tok[kListed];   // first token of each half, -1: none
+  int row[kListed];
+  float ks[kListed], vs[kListed];  // scales of its block (next to each other)
 };
 
-struct ChunkQ8 {
-  U4 k[2][2];     // [half][bytes 16 r and 64 + 16 r of token c]
-  uint2 v[8];     // bytes 8 c of tokens 4 r + j of half 0 (j < 4) and half 1
-  float scale;    // lanes of r = 0, 1: key scales of the halves; r = 2, 3: value scales
-};
+// w 2^k: the largest w of a head is made 2^kTop .. 2^(kTop + 1) and may grow to
+// 2^kMost (fp16 ends below 2^16) before k changes.
+constexpr int kTop = 11, kMost = 15;
 
 // Eight codes as bf16.
 template <int kFmt>
@@ -88,29 +110,24 @@ __device__ __forceinline__ bf16x8_t codes_bf16(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(bf16x8_t, out);
 }
 
-// Dims 4 e .. 4 e + 3 of the lane's eight tokens (words w[0 .. 7]), transposed:
-// out[d] holds the eight tokens' values of dim d.
+// Four dims of the lane's eight tokens (words w[0 .. 7]), transposed: out[d]
+// holds the eight tokens' values of dim d as fp16.
 template <int kFmt>
-__device__ __forceinline__ void transpose_bf16(const uint32_t (&w)[8], bf16x8_t (&out)[4]) {
+__device__ __forceinline__ void transpose_f16(const uint32_t (&w)[8], f16x8_t (&out)[4]) {
   uint32_t o[4][4];
-  if constexpr (kFmt == RESA_Q8_INT8) {
 #pragma unroll
-    for (int t = 0; t < 8; t += 2) {
+  for (int t = 0; t < 8; t += 2) {
+    if constexpr (kFmt == RESA_Q8_INT8) {
       float x[4], y[4];
       codes_f32<kFmt>(w[t], x);
       codes_f32<kFmt>(w[t + 1], y);
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
-        o[d][t / 2] = __builtin_amdgcn_perm(__float_as_uint(y[d]), __float_as_uint(x[d]), 0x07060302u);
-    }
-  } else {
-#pragma unroll
-    for (int t = 0; t < 8; t += 2) {
-      auto pair = [&](int u, bool hi) {
-        return hi ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[u], 1.f, true))
-                  : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[u], 1.f, false));
-      };
-      const uint32_t x0 = pair(t, false), x1 = pair(t, true), y0 = pair(t + 1, false), y1 = pair(t + 1, true);
+      for (int d = 0; d < 4; ++d) o[d][t / 2] = pack_f16_exact(x[d], y[d]);
+    } else {
+      const uint32_t x0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[t], 1.f, false));
+      const uint32_t x1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[t], 1.f, true));
+      const uint32_t y0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[t + 1], 1.f, false));
+      const uint32_t y1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[t + 1], 1.f, true));
       o[0][t / 2] = __builtin_amdgcn_perm(y0, x0, 0x05040100u);
       o[1][t / 2] = __builtin_amdgcn_perm(y0, x0, 0x07060302u);
       o[2][t / 2] = __builtin_amdgcn_perm(y1, x1, 0x05040100u);
@@ -118,20 +135,20 @@ __device__ __forceinline__ void transpose_bf16(const uint32_t (&w)[8], bf16x8_t 
     }
   }
 #pragma unroll
-  for (int d = 0; d < 4; ++d) out[d] = __builtin_bit_cast(bf16x8_t, U4{o[d][0], o[d][1], o[d][2], o[d][3]});
+  for (int d = 0; d < 4; ++d) out[d] = __builtin_bit_cast(f16x8_t, U4{o[d][0], o[d][1], o[d][2], o[d][3]});
 }
 
 __device__ __forceinline__ f32x4_t mfma16(bf16x8_t a, bf16x8_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-template <int G, int BS, int kFmt, int NW, int kDepth>
+template <int G, int BS, int kFmt, int NW>
 __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float* k_scale, const float* v_scale, int bb,
                                                 int hk, int split, DecodeQ8Lds<G, NW>& lds) {
   constexpr int HPB = BS / 16;  // halves per block
   constexpr int kLog2 = BS == 16 ? 4 : BS == 32 ? 5 : 6;
   constexpr int NT = 64 * NW;
-  constexpr int kPer = kIdxBatch / NT;
+  constexpr int kPer = kListed / NT;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int S = a.num_splits;
@@ -145,7 +162,7 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
   const int32_t* idx = a.block_idx + grp * a.n_cap;
   int blkv[kPer];
   auto load_ids = [&](int hb) {
-    const int lim = min(slots, hb + kIdxBatch) - hb;
+    const int lim = min(slots, hb + kListed) - hb;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const int i = tid + j * NT;
@@ -171,8 +188,10 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
   const size_t gbase = paged ? 0 : grp * (size_t)a.c.capacity * kHeadDim;
   const uint8_t* kp = wave_uniform(reinterpret_cast<const uint8_t*>(a.c.k) + gbase);
   const uint8_t* vp = wave_uniform(reinterpret_cast<const uint8_t*>(a.c.v) + gbase);
-  // This lane's scale: of half r % 2, the key's or the value's.
-  const float* sp = (r < 2 ? k_scale : v_scale) + (paged ? 0 : grp * a.c.max_blocks);
+  // Scales from the group's (paged: the pool's) first block on.
+  const size_t sbase = paged ? 0 : grp * a.c.max_blocks;
+  const int sbytes = 4 * (paged ? a.c.num_pages * a.c.kv_heads : a.c.max_blocks);
+  const i32x4_t rks = rsrc_words(k_scale + sbase, sbytes), rvs = rsrc_words(v_scale + sbase, sbytes);
   const float scale = a.scale_log2;
   const float ninf = -__builtin_inff();
   const int n_raw = __hip_atomic_load(a.num_sel + grp, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -183,51 +202,56 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
   const int halves = n * HPB;
   const int valid = 2 * count_below((halves + 1) / 2);  // this split's halves
 
-  auto load_chunk = [&](ChunkQ8& ch, int row0, int row1) __attribute__((always_inline)) {
-    constexpr int kBytes = 16 * kHeadDim;
+  // A half's codes of K and of V into LDS: 16-byte piece p of row t sits in
+  // slot p ^ (t / 2) of K's rows, so that the reads below (one piece of 16
+  // rows) meet every bank once, and in slot p of V's (whole rows).
+  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr(lds.ring[wave]));
+  const int lrow = lane >> 3, lslot = lane & 7;
+  const uint32_t k_off = lrow * kHeadDim + 16 * (lslot ^ (lrow >> 1));
+  const uint32_t k_off8 = (8 + lrow) * kHeadDim + 16 * (lslot ^ (4 + (lrow >> 1)));
+  const uint32_t v_off = 16 * lane;
+  // With `there` false nothing is fetched (zeros arrive), so that the number of
+  // loads on their way is always the same.
+  auto load_chunk = [&](int slot, int row0, int row1, bool there) __attribute__((always_inline)) {
+    const uint32_t to = ring + slot * kChunkBytes;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const size_t base = (size_t)(h == 0 ? row0 : row1) * kHeadDim;
-      const __amdgpu_buffer_rsrc_t rk =
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(kp + base), (short)0, kBytes, kBufWord3);
-      const __amdgpu_buffer_rsrc_t rv =
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(vp + base), (short)0, kBytes, kBufWord3);
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        ch.k[h][e] = __builtin_bit_cast(U4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                rk, c * kHeadDim + 16 * r + 64 * e, 0, kPolicyNt));
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        ch.v[4 * h + j] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(
-                                                        rv, (4 * r + j) * kHeadDim + 8 * c, 0, kPolicyNt));
+      lds_load_rows8<true>(to + h * kHalfBytes, k_off, k_off8, rsrc_words(kp + base, there ? kHalfBytes : 0));
+      lds_load_rows8<true>(to + (2 + h) * kHalfBytes, v_off, v_off + 1024, rsrc_words(vp + base, there ? kHalfBytes : 0));
     }
-    ch.scale = sp[((r & 1) == 0 ? row0 : row1) >> kLog2];
   };
 
-  // Head c % 8: softmax reference m (the same in the four lanes of a column)
-  // and this lane's share l of the sum of the weights.
+  // Head c % 8: softmax reference m and unit 2^-k of w (the same in the four
+  // lanes of a column and in columns c and c ^ 8), and this lane's share l of
+  // the sum of the weights.
   float m = ninf, l = 0.f;
-  f32x4_t o[8];
+  int k = 0;
+  bool none = true;  // no weight met yet: k says nothing
+  f32x4_t o[8];      // in units of 2^-k
 #pragma unroll
   for (int d = 0; d < 8; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  auto consume = [&](ChunkQ8& ch, int t0, int t1) __attribute__((always_inline)) {
-    float x[8], vs[2];
+  typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4;
+  typedef __attribute__((address_space(3))) const u32x2_t lds_u32x2;
+  auto consume = [&](const u32x4_t (&kk)[2][2], u32x2_t (&vv)[8], int t0, int t1, float ks0, float ks1, float vs0,
+                     float vs1) __attribute__((always_inline)) {
+    float x[8], vs[2] = {vs0, vs1};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+      // A scale of the block that is not finite makes its scores NaN.
+      const float kscaled = (finite_f(vs[h]) && finite_f(h == 0 ? ks0 : ks1) ? (h == 0 ? ks0 : ks1) : __builtin_nanf("")) * scale;
       f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        s = mfma16(codes_bf16<kFmt>(ch.k[h][e].x, ch.k[h][e].y), q[2 * e], s);
-        s = mfma16(codes_bf16<kFmt>(ch.k[h][e].z, ch.k[h][e].w), q[2 * e + 1], s);
+        s = mfma16(codes_bf16<kFmt>(kk[h][e][0], kk[h][e][1]), q[2 * e], s);
+        s = mfma16(codes_bf16<kFmt>(kk[h][e][2], kk[h][e][3]), q[2 * e + 1], s);
       }
-      const float ks = scale * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__float_as_int(ch.scale), 16 * h));
-      vs[h] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__float_as_int(ch.scale), 32 + 16 * h));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         // Rounded here, as the reference that is taken of it (a product
         // contracted with the subtraction below could exceed it by far).
-        x[4 * h + i] = s[i] * ks;
+        x[4 * h + i] = s[i] * kscaled;
         __asm__("" : "+v"(x[4 * h + i]));
       }
     }
@@ -240,13 +264,13 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
         const int t = j < 4 ? t0 : t1;
         if (t < 0 || t + 4 * r + (j & 3) >= L) {
           x[j] = ninf;
-          ch.v[j] = uint2{0u, 0u};
+          vv[j] = u32x2_t{0u, 0u};
         }
       }
       if (t0 < 0) vs[0] = 0.f;
       if (t1 < 0) vs[1] = 0.f;
     }
-    float cm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    const float cm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     // The reference moves only when a score exceeds it by more than
     // kRefSlack, so the reduction over the column and the rescale are rare.
     if (__any(cm > m + kRefSlack)) {
@@ -256,45 +280,58 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
       for (int d = 0; d < 8; ++d) o[d] *= alpha;
     }
     const float mref = m == ninf ? 0.f : m;
-    float p[8];
+    float p[8], w[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) p[j] = fast_exp2(x[j] - mref);
     l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-    uint32_t b1[8], b2[8];
+    float f[2] = {__builtin_ldexpf(vs[0], k), __builtin_ldexpf(vs[1], k)}, wm = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      float w = p[j] * vs[j >> 2];
-      if (partial) w = x[j] == ninf ? 0.f : w;
-      const float r1 = w - __uint_as_float(__float_as_uint(w) & 0xffff0000u);
-      const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
-      b1[j] = __float_as_uint(c < 8 ? w : r1);
-      b2[j] = __float_as_uint(c < 8 ? r2 : 0.f);
+      w[j] = p[j] * f[j >> 2];
+      wm = fmaxf(wm, w[j]);
     }
-    U4 f1, f2;
-    f1 = U4{__builtin_amdgcn_perm(b1[1], b1[0], 0x07060302u), __builtin_amdgcn_perm(b1[3], b1[2], 0x07060302u),
-            __builtin_amdgcn_perm(b1[5], b1[4], 0x07060302u), __builtin_amdgcn_perm(b1[7], b1[6], 0x07060302u)};
-    f2 = U4{__builtin_amdgcn_perm(b2[1], b2[0], 0x07060302u), __builtin_amdgcn_perm(b2[3], b2[2], 0x07060302u),
-            __builtin_amdgcn_perm(b2[5], b2[4], 0x07060302u), __builtin_amdgcn_perm(b2[7], b2[6], 0x07060302u)};
-    const bf16x8_t p1 = __builtin_bit_cast(bf16x8_t, f1), p2 = __builtin_bit_cast(bf16x8_t, f2);
+    if (__any(none || wm >= (float)(1 << kMost))) {
+      float y = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y = fmaxf(y, p[j] * vs[j >> 2]);
+      y = max_xor32(max_xor16(y));
+      const int want = kTop + 127 - (int)((__float_as_uint(y) >> 23) & 0xffu);
+      const int to = !(y > 0.f) ? k : none ? want : min(k, want);
+      none = none && !(y > 0.f);
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[d][i] = __builtin_ldexpf(o[d][i], to - k);
+      k = to;
+      f[0] = __builtin_ldexpf(vs[0], k);
+      f[1] = __builtin_ldexpf(vs[1], k);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = p[j] * f[j >> 2];
+    }
+    f16x8_t ph;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const _Float16 first = (_Float16)w[j];
+      ph[j] = c < 8 ? first : (_Float16)(w[j] - (float)first);
+    }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      uint32_t w[8];
+      uint32_t words[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = e == 0 ? ch.v[j].x : ch.v[j].y;
-      bf16x8_t vt[4];
-      transpose_bf16<kFmt>(w, vt);
+      for (int j = 0; j < 8; ++j) words[j] = vv[j][e];
+      f16x8_t vt[4];
+      transpose_f16<kFmt>(words, vt);
 #pragma unroll
-      for (int d = 0; d < 4; ++d) o[4 * e + d] = mfma16(vt[d], p1, o[4 * e + d]);
-#pragma unroll
-      for (int d = 0; d < 4; ++d) o[4 * e + d] = mfma16(vt[d], p2, o[4 * e + d]);
+      for (int d = 0; d < 4; ++d)
+        o[4 * e + d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt[d], ph, o[4 * e + d], 0, 0, 0);
     }
   };
 
   int hb = 0;
   do {
     if (hb > 0) load_ids(hb);
-    const int he = min(valid, hb + kIdxBatch);
-    const int lim = min(slots, hb + kIdxBatch) - hb;
+    const int he = min(valid, hb + kListed);
+    const int lim = min(slots, hb + kListed) - hb;
     int tk[kPer], rw[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -326,41 +363,58 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
         lds.row[i] = tk[j] < 0 ? 0 : rw[j];
       }
     }
-    lds_sync();
-    // Chunk cc of the pass: halves 2 cc and 2 cc + 1. Wave w takes chunks
-    // w, w + NW, ...; kDepth + 1 buffers, as in the bf16 decode.
-    const int chunks = (he - hb) / 2;
-    auto tok = [&](int cc, int h) -> int {
-      return cc < chunks ? __builtin_amdgcn_readfirstlane(lds.tok[2 * cc + h]) : -1;
-    };
-    auto row = [&](int cc, int h) -> int { return __builtin_amdgcn_readfirstlane(lds.row[2 * cc + h]); };
-    ChunkQ8 ring[kDepth + 1];
-    int tring[kDepth + 1][2];
-    int cc = wave;
+    // Scales straight into their lists (lane i's lands at 4 i), in front of the
+    // codes.
+    const uint32_t list = __builtin_amdgcn_readfirstlane(lds_addr(lds.ks)) + 4 * 64 * wave;
 #pragma unroll
-    for (int k = 0; k <= kDepth; ++k) {
-      tring[k][0] = tok(cc + k * NW, 0);
-      tring[k][1] = tok(cc + k * NW, 1);
-      if (cc + k * NW < chunks) load_chunk(ring[k], row(cc + k * NW, 0), row(cc + k * NW, 1));
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    while (cc < chunks) {
-#pragma unroll
-      for (int k = 0; k <= kDepth; ++k) {
-        if (cc < chunks) {
-          consume(ring[k], tring[k][0], tring[k][1]);
-          __builtin_amdgcn_sched_barrier(0);
-          const int next = cc + (kDepth + 1) * NW;
-          tring[k][0] = tok(next, 0);
-          tring[k][1] = tok(next, 1);
-          if (next < chunks) load_chunk(ring[k], row(next, 0), row(next, 1));
-          __builtin_amdgcn_sched_barrier(0);
-          cc += NW;
-        }
+    for (int j = 0; j < kPer; ++j) {
+      if (j * NT < lim) {
+        const uint32_t at = 4 * (tk[j] < 0 ? 0 : rw[j] >> kLog2);
+        lds_load_dword(list + 4 * j * NT, at, rks);
+        lds_load_dword(list + 4 * (j * NT + kListed), at, rvs);
       }
     }
     lds_sync();
-    hb += kIdxBatch;
+    // Chunk cc of the pass: halves 2 cc and 2 cc + 1. Wave w takes chunks w,
+    // w + NW, ...
+    const int chunks = (he - hb) / 2;
+    auto ask = [&](int slot, int cc) __attribute__((always_inline)) {
+      const bool there = cc < chunks;
+      const int at = there ? 2 * cc : 0;
+      load_chunk(slot, __builtin_amdgcn_readfirstlane(lds.row[at]), __builtin_amdgcn_readfirstlane(lds.row[at + 1]), there);
+    };
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) ask(i, wave + i * NW);
+    __builtin_amdgcn_s_waitcnt(wait_vm(kChunkLoads * kRing));
+    lds_sync();
+    int slot = 0;
+#pragma unroll 1
+    for (int cc = wave; cc < chunks; cc += NW) {
+      const int t0 = __builtin_amdgcn_readfirstlane(lds.tok[2 * cc]), t1 = __builtin_amdgcn_readfirstlane(lds.tok[2 * cc + 1]);
+      const float ks0 = lds.ks[2 * cc], ks1 = lds.ks[2 * cc + 1], vs0 = lds.vs[2 * cc], vs1 = lds.vs[2 * cc + 1];
+      __builtin_amdgcn_s_waitcnt(wait_vm(kChunkLoads * (kRing - 1)));
+      compiler_fence();
+      const uint32_t at = ring + slot * kChunkBytes;
+      u32x4_t kk[2][2];
+      u32x2_t vv[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          kk[h][e] = *(lds_u32x4*)(uintptr_t)(at + h * kHalfBytes + c * kHeadDim + 16 * ((4 * e + r) ^ (c >> 1)));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          vv[4 * h + j] = *(lds_u32x2*)(uintptr_t)(at + (2 + h) * kHalfBytes + (4 * r + j) * kHeadDim + 8 * c);
+      }
+      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);  // read before the slot is filled again
+      compiler_fence();
+      ask(slot, cc + kRing * NW);
+      consume(kk, vv, t0, t1, ks0, ks1, vs0, vs1);
+      slot = slot + 1 == kRing ? 0 : slot + 1;
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+    lds_sync();
+    hb += kListed;
   } while (hb < valid);
 
   __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
@@ -368,13 +422,16 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
   if (S > 1 && tid == 0)
     ticket = __hip_atomic_fetch_add(a.counters + grp, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 
-  // The wave's state to LDS: the three terms' products are added (columns c
-  // and c ^ 8), dims 8 (4 r + i) + d.
+  // The wave's state to LDS: the terms' products are added (columns c and
+  // c ^ 8), dims 8 (4 r + i) + d.
   const float lt = sum_xor32(sum_xor16(l));
 #pragma unroll
   for (int d = 0; d < 8; ++d)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[d][i] += dpp<kDppRor8>(o[d][i]);
+    for (int i = 0; i < 4; ++i) {
+      const float y = __builtin_ldexpf(o[d][i], -k);
+      o[d][i] = y + dpp<kDppRor8>(y);
+    }
   if (c < G) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -419,10 +476,10 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
 }
 
 template <int G, int BS, int kFmt>
-__global__ __launch_bounds__(64 * kDecodeWaves) void k_decode_q8(DecodeArgs a, const float* k_scale,
-                                                                 const float* v_scale) {
+__global__ __launch_bounds__(64 * kDecodeWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_decode_q8(
+    DecodeArgs a, const float* k_scale, const float* v_scale) {
   __shared__ DecodeQ8Lds<G, kDecodeWaves> lds;
-  decode_split_q8<G, BS, kFmt, kDecodeWaves, kDecodeDepth>(a, k_scale, v_scale, blockIdx.z, blockIdx.y, blockIdx.x, lds);
+  decode_split_q8<G, BS, kFmt, kDecodeWaves>(a, k_scale, v_scale, blockIdx.z, blockIdx.y, blockIdx.x, lds);
 }
 
 template <int G, int kFmt>
@@ -455,9 +512,11 @@ hipError_t launch_fmt(const DecodeArgs& a, const float* ks, const float* vs, hip
 }  // namespace
 
 int32_t decode_q8_auto_splits(int32_t batch, int32_t kv_heads, int32_t n_cap, int32_t block_size) {
+  // At most a workgroup per CU (6 sequences of 50K, 48 groups: 18.0 us with 5
+  // splits, 18.1 with 6, 22.8 with 12), with a chunk per wave at least.
   const int64_t groups = (int64_t)batch * kv_heads;
   const int64_t chunks = ((int64_t)n_cap * block_size + 31) / 32;
-  int64_t s = (256 + groups - 1) / groups;
+  int64_t s = 256 / groups;
   const int64_t most = chunks / kDecodeWaves;
   if (s > most) s = most;
   if (s > 256) s = 256;

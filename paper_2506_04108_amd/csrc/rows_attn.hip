@@ -61,7 +61,6 @@ typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kRowsPerWave = 32;
@@ -77,29 +76,8 @@ constexpr int kPacked = -1;                // source of keys: packed bf16 rows, 
 // (4 aligned rows, four neighbouring pieces) free of bank conflicts.
 __host__ __device__ constexpr int swz(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
 
-constexpr int kWaitVm0 = 0x0F70, kWaitLgkm0 = 0xC07F;
+constexpr int kWaitVm0 = kWaitVmcnt0;
 
-__device__ __forceinline__ i32x4_t rsrc_words(const void* p, int bytes) {
-  const uint64_t u = reinterpret_cast<uint64_t>(p);
-  return i32x4_t{(int32_t)__builtin_amdgcn_readfirstlane((uint32_t)u),
-                 (int32_t)(__builtin_amdgcn_readfirstlane((uint32_t)(u >> 32)) & 0xffffu),
-                 __builtin_amdgcn_readfirstlane(bytes), kBufWord3};
-}
-__device__ __forceinline__ uint32_t lds_addr(const void* p) {
-  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-// A wave's eight rows of a tile straight into LDS: lane i's 16 bytes at offset
-// voff0 (voff1) of the resource land at lds + 16 i (lds + 1024 + 16 i). The
-// completion is ordered by hand (vmcnt 0, then a barrier). M0 is restored.
-__device__ __forceinline__ void lds_load_rows8(uint32_t lds, uint32_t voff0, uint32_t voff1, i32x4_t rk) {
-  uint32_t saved;
-  __asm__ volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
-      "s_add_i32 m0, %1, 1024\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved) : "s"(lds), "v"(voff0), "v"(voff1), "s"(rk) : "memory", "scc");
-}
 // 1 or 2 KB of codes likewise.
 template <int kUnits>
 __device__ __forceinline__ void lds_load_codes(uint32_t lds, uint32_t voff, i32x4_t rk) {
@@ -114,11 +92,6 @@ __device__ __forceinline__ void lds_load_codes(uint32_t lds, uint32_t voff, i32x
         : "=&s"(saved) : "s"(lds), "v"(voff), "s"(rk) : "memory");
   }
 }
-// Two fp32 values that are fp16 values, packed.
-__device__ __forceinline__ uint32_t pack_f16_exact(float lo, float hi) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
-}
-__device__ __forceinline__ void compiler_fence() { __asm__ volatile("" ::: "memory"); }
 __device__ __forceinline__ void bare_barrier() {
   compiler_fence();
   __builtin_amdgcn_s_barrier();
@@ -135,7 +108,6 @@ __device__ __forceinline__ float sub_rounded(float x, float y) {
   __asm__ volatile("" : "+v"(x));
   return x - y;
 }
-__device__ __forceinline__ bool finite_f(float x) { return fabsf(x) < __builtin_inff(); }
 // Whether one of the two bf16 values of a word is infinite or NaN.
 __device__ __forceinline__ bool not_finite2(uint32_t w) {
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;

@@ -14,6 +14,58 @@ namespace resa {
 typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+
+// s_waitcnt immediates: LDS operations done; at most n (< 64) vector loads out.
+constexpr int kWaitLgkm0 = 0xC07F;
+constexpr int wait_vm(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0F70; }
+
+// Words of a buffer resource over `bytes` bytes at p (stride 0, 32-bit format),
+// both the same in every lane. Offsets at or past `bytes` read as zero.
+__device__ __forceinline__ i32x4_t rsrc_words(const void* p, int bytes) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  return i32x4_t{(int32_t)__builtin_amdgcn_readfirstlane((uint32_t)u),
+                 (int32_t)(__builtin_amdgcn_readfirstlane((uint32_t)(u >> 32)) & 0xffffu),
+                 __builtin_amdgcn_readfirstlane(bytes), kBufWord3};
+}
+// LDS byte address of an LDS object.
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+// A wave's eight rows of a tile straight into LDS: lane i's 16 bytes at offset
+// voff0 (voff1) of the resource land at lds + 16 i (lds + 1024 + 16 i). The
+// completion is ordered by hand (vmcnt 0, then a barrier). M0 is restored.
+template <bool kNt = false>
+__device__ __forceinline__ void lds_load_rows8(uint32_t lds, uint32_t voff0, uint32_t voff1, i32x4_t rk) {
+  uint32_t saved;
+  if constexpr (kNt)
+    __asm__ volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %4, 0 offen nt lds\n\t"
+        "s_add_i32 m0, %1, 1024\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen nt lds\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved) : "s"(lds), "v"(voff0), "v"(voff1), "s"(rk) : "memory", "scc");
+  else
+    __asm__ volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+        "s_add_i32 m0, %1, 1024\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved) : "s"(lds), "v"(voff0), "v"(voff1), "s"(rk) : "memory", "scc");
+}
+// One dword a lane likewise, at offset voff of the resource: lane i's lands at
+// lds + 4 i.
+__device__ __forceinline__ void lds_load_dword(uint32_t lds, uint32_t voff, i32x4_t rk) {
+  uint32_t saved;
+  __asm__ volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved) : "s"(lds), "v"(voff), "s"(rk) : "memory");
+}
+// Keeps the compiler from moving memory accesses across this point.
+__device__ __forceinline__ void compiler_fence() { __asm__ volatile("" ::: "memory"); }
+
 // Largest magnitude of a code value.
 template <int kFmt>
 struct Q8 {
@@ -27,6 +79,12 @@ constexpr float kQ8Least = 7.888609052210118e-31f;
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, bf16x2v_t{(__bf16)lo, (__bf16)hi});
 }
+
+// Two fp32 values that are fp16 values, packed.
+__device__ __forceinline__ uint32_t pack_f16_exact(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+}
+__device__ __forceinline__ bool finite_f(float x) { return fabsf(x) < __builtin_inff(); }
 
 // The four codes of a word as fp32, exactly.
 template <int kFmt>
