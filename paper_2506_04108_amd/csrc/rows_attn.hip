@@ -68,6 +68,7 @@ constexpr int kKT = 64;                    // keys per tile
 constexpr int kKT32 = kKT / 32, kKT16 = kKT / 16;
 constexpr int kRowBytes = kHeadDim * 2;
 constexpr int kCus = 256;
+constexpr int64_t kLongSplit = 1024;      // keys of a split that is long
 constexpr float kMaxWeightSum = 4096.f;
 constexpr int kPacked = -1;                // source of keys: packed bf16 rows, else the format of the 8-bit cache
 
@@ -134,55 +135,68 @@ __device__ __forceinline__ SeqRows seq_rows(const RowsArgs& a, int s) {
 // in units of a block's rows: block b of a sequence with h rows' worth of
 // earlier keys costs h + b + 1. The cost of item i is the largest x with more
 // than i blocks of cost >= x; among the blocks of that cost the sequences come
-// in order.
-template <int kSrc>
-__device__ __forceinline__ bool find_block(const RowsArgs& a, int item, int per, int& seq, int& qblk) {
+// in order. The first 64 sequences' counts stay in registers, so that up to
+// there the search reads memory once.
+template <int kSrc, int kPer>
+__device__ __forceinline__ bool find_block(const RowsArgs& a, int item, SeqRows& sr, int& seq, int& qblk) {
   const int lane = threadIdx.x & 63;
-  const int G = a.group;
-  auto blocks = [&](int s, int& h) -> int {
-    h = 0;
-    if (s >= a.batch) return 0;
-    const SeqRows q = seq_rows<kSrc>(a, s);
-    if (kSrc != kPacked) h = (int)((int64_t)(q.L - q.n) * G / per);
-    return (int)(((int64_t)q.n * G + per - 1) / per);
+  auto earlier = [&](const SeqRows& q) -> int {
+    return kSrc == kPacked ? 0 : (int)((int64_t)(q.L - q.n) * a.group / kPer);
   };
-  int h0;
-  const int nb0 = blocks(lane, h0);  // the first 64 sequences' stay in registers
-  auto at_least = [&](int x) -> int {  // blocks of cost >= x
-    int c = min(max(h0 + nb0 - x + 1, 0), nb0);
+  auto blocks = [&](const SeqRows& q) -> int { return (int)(((int64_t)q.n * a.group + kPer - 1) / kPer); };
+  auto rows_at = [&](int s) -> SeqRows { return s < a.batch ? seq_rows<kSrc>(a, s) : SeqRows{0, 0, 0}; };
+  const SeqRows q0 = rows_at(lane);
+  const int h0 = earlier(q0), nb0 = blocks(q0);
+  int lo, rank = 0;
+  seq = 0;
+  if (a.batch == 1) {
+    const int h = __builtin_amdgcn_readlane(h0, 0), nb = __builtin_amdgcn_readlane(nb0, 0);
+    if (nb <= item) return false;
+    lo = h + nb - item;
+  } else {
+    auto at_least = [&](int x) -> int {  // blocks of cost >= x
+      int c = min(max(h0 + nb0 - x + 1, 0), nb0);
+      for (int base = 64; base < a.batch; base += 64) {
+        const SeqRows q = rows_at(base + lane);
+        const int nb = blocks(q);
+        c += min(max(earlier(q) + nb - x + 1, 0), nb);
+      }
+      return wave_total(c);
+    };
+    int most = nb0 == 0 ? 0 : h0 + nb0, least = nb0 == 0 ? INT32_MAX : h0 + 1;
     for (int base = 64; base < a.batch; base += 64) {
-      int h;
-      const int nb = blocks(base + lane, h);
-      c += min(max(h + nb - x + 1, 0), nb);
+      const SeqRows q = rows_at(base + lane);
+      const int h = earlier(q), nb = blocks(q);
+      if (nb > 0) {
+        most = max(most, h + nb);
+        least = min(least, h + 1);
+      }
     }
-    return wave_total(c);
-  };
-  int most = h0 + nb0;
-  for (int base = 64; base < a.batch; base += 64) {
-    int h;
-    const int nb = blocks(base + lane, h);
-    most = max(most, h + nb);
-  }
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) most = max(most, __shfl_xor(most, d));
-  most = __builtin_amdgcn_readfirstlane(most);
-  if (at_least(1) <= item) return false;
-  int lo = 1, hi = most + 1;  // more than `item` blocks of cost >= lo, not of cost >= hi
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (at_least(mid) > item) lo = mid;
-    else hi = mid;
+    for (int d = 1; d < 64; d *= 2) {
+      most = max(most, __shfl_xor(most, d));
+      least = min(least, __shfl_xor(least, d));
+    }
+    most = __builtin_amdgcn_readfirstlane(most);
+    lo = __builtin_amdgcn_readfirstlane(least);
+    if (at_least(1) <= item) return false;
+    int hi = most + 1;  // more than `item` blocks of cost >= lo, not of cost >= hi
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (at_least(mid) > item) lo = mid;
+      else hi = mid;
+    }
+    auto of_cost = [&](int s) -> int {
+      const SeqRows q = s < 64 ? q0 : rows_at(s);
+      const int h = earlier(q);
+      return lo > h && lo <= h + blocks(q) ? 1 : 0;
+    };
+    if (!find_seq(item - at_least(lo + 1), a.batch, of_cost, seq, rank)) return false;
   }
-  int rank;
-  auto of_cost = [&](int s) -> int {
-    int h;
-    const int nb = blocks(s, h);
-    return lo > h && lo <= h + nb ? 1 : 0;
-  };
-  if (!find_seq(item - at_least(lo + 1), a.batch, of_cost, seq, rank)) return false;
-  int h;
-  blocks(seq, h);
-  qblk = lo - h - 1;
+  sr = seq < 64 ? SeqRows{__builtin_amdgcn_readlane(q0.first, seq & 63), __builtin_amdgcn_readlane(q0.n, seq & 63),
+                          __builtin_amdgcn_readlane(q0.L, seq & 63)}
+                : seq_rows<kSrc>(a, seq);
+  qblk = lo - earlier(sr) - 1;
   return true;
 }
 
@@ -203,15 +217,14 @@ struct RowsLds<kStages, true> {
   uint8_t raw[2][kKT * kHeadDim];
 };
 
-// Packed rows, 8 waves: one workgroup a CU, four stages of K and V. Otherwise
-// two stages, and with 4 waves two workgroups a CU. A barrier every kBar
-// tiles, half the stages.
-template <int kWaves, int kSrc, bool kPaged>
+// With four stages of K and V (packed rows) one workgroup fits a CU, with two
+// stages and four waves two do. A barrier every kBar tiles, half the stages.
+template <int kWaves, int kStages, int kSrc, bool kPaged>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_rows_attn(RowsArgs a) {
   constexpr bool kQ8 = kSrc != kPacked;
   // Weights and V: bf16, or over codes fp16.
   typedef std::conditional_t<kQ8, f16x8_t, bf16x8_t> P8;
-  constexpr int kStages = kWaves == 8 && !kQ8 ? 4 : 2, kBar = kStages / 2;
+  constexpr int kBar = kStages / 2;
   constexpr int kLoadRows = kKT / kWaves;  // tile rows whose K and V each wave brings in
   constexpr int kUnits = kLoadRows / 8;
   constexpr int kRowsPerWg = kRowsPerWave * kWaves;
@@ -219,14 +232,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   typedef RowsLds<kStages, kQ8> Lds;
   __shared__ __attribute__((aligned(1024))) Lds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int hk = blockIdx.x % a.kv_heads;
-  const int S = a.num_splits;
-  const int rest = blockIdx.x / a.kv_heads;
-  const int split = rest % S;
+  const int S = a.num_splits, G = a.group;
+  const int hk = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % S;
   int seq, qblk;
-  if (!find_block<kSrc>(a, rest / S, kRowsPerWg, seq, qblk)) return;
-  const SeqRows sr = seq_rows<kSrc>(a, seq);
-  const int G = a.group, R = sr.n * G, past = sr.L - sr.n;
+  SeqRows sr;
+  if (!find_block<kSrc, kRowsPerWg>(a, rest / S, sr, seq, qblk)) return;
+  if constexpr (!kQ8) {
+    if (tid == 0) lds.odd = 0;
+  }
+  const int R = sr.n * G, past = sr.L - sr.n;
   const int k0 = split * a.chunk;
   const int last_row = min(R - 1, (qblk + 1) * kRowsPerWg - 1);
   const int k1 = min(min(k0 + a.chunk, sr.L), past + last_row / G + 1);
@@ -298,18 +312,44 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   };
 
   // Q^T (B of S^T): lane holds row lq, dims 16 s + 8 hi .. + 8 for k-step s.
+  // Rows are read 128 B at a time, eight lanes a row, and change lanes by way of
+  // LDS, a half of the dims after the other: 4 KB of the wave's own in stages
+  // that nothing has been requested into yet. 16 prompts of up to 77 tokens:
+  // 12.4 us with the rows read as the lanes hold them, 32 B each, 11.6 us so.
   bf16x8_t qb[8];
+  U4 qx[2][4];
+  const int qrow = lane >> 3;
   {
-    const int h = rho % G, r = rho / G;
-    const uint16_t* qp = a.q + (int64_t)(sr.first + min(r, sr.n - 1)) * a.q_stride + (hk * G + h) * kHeadDim + 8 * hi;
+    // Row rel of the block's: a quotient of small numbers, exact in fp32.
+    const int r0 = (qblk * kRowsPerWg) / G, h0 = qblk * kRowsPerWg - r0 * G;
+    const float inv_g = 1.f / (float)G;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      U4 x = ld16(qp + 16 * s);
-      if (rho >= R) x = U4{0, 0, 0, 0};
-      qb[s] = __builtin_bit_cast(bf16x8_t, U4{(x.x & q_and) ^ q_xor, (x.y & q_and) ^ q_xor,
-                                             (x.z & q_and) ^ q_xor, (x.w & q_and) ^ q_xor});
+    for (int j = 0; j < 4; ++j) {
+      const int rel = wave * kRowsPerWave + 8 * j + qrow + h0;
+      const int dr = (int)(((float)rel + 0.5f) * inv_g);
+      const uint16_t* qp = a.q + (int64_t)(sr.first + min(r0 + dr, sr.n - 1)) * a.q_stride +
+                           (hk * G + rel - dr * G) * kHeadDim + 8 * (lane & 7);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) qx[p][j] = ld16(qp + 64 * p);
     }
   }
+  auto exchange_q = [&]() __attribute__((always_inline)) {
+    uint8_t* mine = (kQ8 ? lds.k[0] : lds.v[kStages / 2]) + wave * (kRowsPerWave * 128);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = 8 * j + qrow;
+        const U4 x = qx[p][j];
+        st16(mine + r * 128 + 16 * ((lane & 7) ^ ((r >> 1) & 7)),
+             row_base + r < R ? U4{(x.x & q_and) ^ q_xor, (x.y & q_and) ^ q_xor, (x.z & q_and) ^ q_xor, (x.w & q_and) ^ q_xor}
+                              : U4{0, 0, 0, 0});
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        qb[4 * p + s] = __builtin_bit_cast(bf16x8_t, ld16(mine + lq * 128 + 16 * ((2 * s + hi) ^ ((lq >> 1) & 7))));
+    }
+  };
 
   // This wave's rows of tile ti: how many exist below k1.
   auto rows_of = [&](int ti) __attribute__((always_inline)) -> int {
@@ -701,9 +741,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   if constexpr (kQ8) {
     take_window(load_window(0));
     coming = load_window(32);
-  } else if (tid == 0) {
-    lds.odd = 0;
   }
+  // The first tiles of K and V on their way.
+  auto request = [&]() __attribute__((always_inline)) {
+    if constexpr (!kQ8) {
+#pragma unroll
+      for (int t = 0; t <= kBar; ++t) issue_k(t, t);
+#pragma unroll
+      for (int t = 0; t < kBar; ++t) issue_v(t, t);
+    }
+  };
+  request();
+  if constexpr (!kQ8) exchange_q();
   for (;;) {
     if constexpr (kQ8) {
       // K(1) by way of the stage that V(1) has not been put into yet.
@@ -711,17 +760,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       ask(true, 0, raw_at(true));
       ask(false, 0, raw_at(false));
       ask(true, 1, spare);
+      exchange_q();
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
+      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+      bare_barrier();  // codes go where queries were
       put(true, 0, raw_at(true), 0);
       put(false, 0, raw_at(false), 0);
       put(true, 1, spare, 1);
       ask(true, 2, raw_at(true));
       ask(false, 1, raw_at(false));
     } else {
-#pragma unroll
-      for (int t = 0; t <= kBar; ++t) issue_k(t, t);
-#pragma unroll
-      for (int t = 0; t < kBar; ++t) issue_v(t, t);
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
     }
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
@@ -754,6 +802,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     guard = true;
     clear_o();
     l = 0.f;
+    request();
   }
 
   // V values that are not finite, cleared in the second pass: whoever sees
@@ -883,11 +932,11 @@ int64_t most_blocks(const RowsArgs& a, int waves) {
   return (int64_t)a.rows * a.group / (kRowsPerWave * waves) + a.batch;
 }
 
-template <int kWaves, int kSrc, bool kPaged>
+template <int kWaves, int kStages, int kSrc, bool kPaged>
 hipError_t launch_attn(const RowsArgs& a, hipStream_t stream) {
   const int64_t grid = most_blocks(a, kWaves) * a.num_splits * a.kv_heads;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_rows_attn<kWaves, kSrc, kPaged>), dim3((uint32_t)grid), dim3(64 * kWaves), 0, stream, a);
+  hipLaunchKernelGGL((k_rows_attn<kWaves, kStages, kSrc, kPaged>), dim3((uint32_t)grid), dim3(64 * kWaves), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -896,9 +945,9 @@ hipError_t launch_q8(const RowsArgs& a, hipStream_t stream) {
   const bool paged = a.c.table != nullptr;
   hipError_t e;
   if (rows_waves(a.batch, a.rows, a.group) == 4)
-    e = paged ? launch_attn<4, kSrc, true>(a, stream) : launch_attn<4, kSrc, false>(a, stream);
+    e = paged ? launch_attn<4, 2, kSrc, true>(a, stream) : launch_attn<4, 2, kSrc, false>(a, stream);
   else
-    e = paged ? launch_attn<8, kSrc, true>(a, stream) : launch_attn<8, kSrc, false>(a, stream);
+    e = paged ? launch_attn<8, 2, kSrc, true>(a, stream) : launch_attn<8, 2, kSrc, false>(a, stream);
   if (e != hipSuccess || a.num_splits == 1) return e;
   const int64_t outs = (int64_t)a.rows * a.q_heads;
   hipLaunchKernelGGL(k_rows_combine<kSrc>, dim3((uint32_t)((outs + 3) / 4)), dim3(256), 0, stream, a);
@@ -912,25 +961,28 @@ int32_t rows_waves(int32_t batch, int32_t rows, int32_t group) {
   return (int64_t)rows * group <= (int64_t)128 * batch ? 4 : 8;
 }
 
-// Key splits at most: enough for two workgroups a CU (4 waves) or one (8).
-static int64_t rows_most_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows) {
+// Key splits at most: enough for a workgroup on every CU, and for a second one
+// (of 4 waves) where a split stays long: every split writes its rows' sums and
+// the merge reads them again. 32 rows of 32 heads behind 8K: 32.9 us with one
+// workgroup a CU, 40.0 with two; behind 8 x 64K 444 and 384.
+static int64_t rows_most_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
   const int waves = rows_waves(batch, rows, group);
   const int64_t per = kRowsPerWave * waves;
   const int64_t each = ((int64_t)((rows + batch - 1) / batch) * group + per - 1) / per;
   const int64_t wgs = (each < 1 ? 1 : each) * batch * kv_heads;
-  const int64_t want = waves == 4 ? 2 * kCus : kCus;
-  return wgs >= want ? 1 : (want + wgs - 1) / wgs;
+  const auto splits = [&](int64_t want) { return wgs >= want ? 1 : (want + wgs - 1) / wgs; };
+  return waves == 4 && max_seq_len >= kLongSplit * splits(kCus) ? splits(2 * kCus) : splits(kCus);
 }
 
 int32_t rows_chunk(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
-  const int64_t most = rows_most_splits(batch, kv_heads, group, rows);
+  const int64_t most = rows_most_splits(batch, kv_heads, group, rows, max_seq_len);
   int64_t chunk = ((max_seq_len + most - 1) / most + 63) / 64 * 64;
   return (int32_t)(chunk < 128 ? 128 : chunk);
 }
 
 // A bound on the splits that never decreases as the length grows.
 int32_t rows_max_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
-  const int64_t most = rows_most_splits(batch, kv_heads, group, rows);
+  const int64_t most = rows_most_splits(batch, kv_heads, group, rows, max_seq_len);
   const int64_t by_len = ((int64_t)max_seq_len + 127) / 128;
   const int64_t s = by_len < most ? by_len : most;
   return (int32_t)(s < 1 ? 1 : s);
@@ -942,8 +994,8 @@ hipError_t launch_rows_q8(const RowsArgs& a, int32_t format, hipStream_t stream)
 
 hipError_t launch_prompt(const RowsArgs& a, hipStream_t stream) {
   // Small launches in 4-wave workgroups, two a CU.
-  return most_blocks(a, 8) * a.kv_heads < 2 * kCus ? launch_attn<4, kPacked, false>(a, stream)
-                                                   : launch_attn<8, kPacked, false>(a, stream);
+  return most_blocks(a, 8) * a.kv_heads < 2 * kCus ? launch_attn<4, 2, kPacked, false>(a, stream)
+                                                   : launch_attn<8, 4, kPacked, false>(a, stream);
 }
 
 }  // namespace resa
