@@ -172,13 +172,8 @@ __device__ __forceinline__ bool find_block(const RowsArgs& a, int item, SeqRows&
         least = min(least, h + 1);
       }
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      most = max(most, __shfl_xor(most, d));
-      least = min(least, __shfl_xor(least, d));
-    }
-    most = __builtin_amdgcn_readfirstlane(most);
-    lo = __builtin_amdgcn_readfirstlane(least);
+    most = (int)wave_max((uint32_t)most);
+    lo = (int)~wave_max(~(uint32_t)least);
     if (at_least(1) <= item) return false;
     int hi = most + 1;  // more than `item` blocks of cost >= lo, not of cost >= hi
     while (hi - lo > 1) {

@@ -168,6 +168,16 @@ __device__ __forceinline__ int wave_total(int x) {
   return __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)x), 63);
 }
 
+// Maximum over the 64 lanes, uniform.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kDppXor1, 0xf, 0xf, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kDppXor2, 0xf, 0xf, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kDppHalfMirror, 0xf, 0xf, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kDppMirror, 0xf, 0xf, true));
+  return max(max((uint32_t)__builtin_amdgcn_readlane((int)x, 0), (uint32_t)__builtin_amdgcn_readlane((int)x, 16)),
+             max((uint32_t)__builtin_amdgcn_readlane((int)x, 32), (uint32_t)__builtin_amdgcn_readlane((int)x, 48)));
+}
+
 // The block scale's index of logical block m of (sequence, kv head), or -1
 // when the block table sends it outside the pool.
 __device__ __forceinline__ int64_t scale_index(const CacheArgs& c, int bb, int hk, int m) {

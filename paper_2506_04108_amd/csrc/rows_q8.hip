@@ -17,23 +17,35 @@
 namespace resa {
 namespace {
 
-// Items of a wave: blocks that the new rows of a sequence touch.
+// Items of a wave: blocks that the new rows of a sequence touch. The first 64
+// sequences' rows stay in registers, so that up to there the search reads
+// memory once.
 __device__ __forceinline__ bool find_block(const RowsQ8Args& a, int item, int log2_block, int& bb, int& m, int& first_row,
                                            int& first, int& L) {
-  const int b1 = (1 << log2_block) - 1;
-  int rank;
-  auto count = [&](int s) -> int {
-    int at, n;
-    packed_rows(a.cu, a.rows, s, at, n);
-    const int len = a.seq_lens[s];
-    if (n == 0 || len < n || len > a.c.capacity) return 0;
-    return ((len + b1) >> log2_block) - ((len - n) >> log2_block);
+  struct Seq {
+    int at, n, len;
   };
+  const int lane = threadIdx.x & 63, b1 = (1 << log2_block) - 1;
+  auto rows_at = [&](int s) -> Seq {
+    Seq q;
+    packed_rows(a.cu, a.rows, s, q.at, q.n);
+    q.len = a.seq_lens[s];
+    return q;
+  };
+  const Seq q0 = lane < a.c.batch ? rows_at(lane) : Seq{0, 0, 0};
+  auto count = [&](int s) -> int {
+    const Seq q = s < 64 ? q0 : rows_at(s);
+    if (q.n == 0 || q.len < q.n || q.len > a.c.capacity) return 0;
+    return ((q.len + b1) >> log2_block) - ((q.len - q.n) >> log2_block);
+  };
+  int rank;
   if (!find_seq(item, a.c.batch, count, bb, rank)) return false;
-  int n;
-  packed_rows(a.cu, a.rows, bb, first_row, n);
-  L = a.seq_lens[bb];
-  first = L - n;
+  const Seq q = bb < 64 ? Seq{__builtin_amdgcn_readlane(q0.at, bb & 63), __builtin_amdgcn_readlane(q0.n, bb & 63),
+                              __builtin_amdgcn_readlane(q0.len, bb & 63)}
+                        : rows_at(bb);
+  first_row = q.at;
+  L = q.len;
+  first = L - q.n;
   m = (first >> log2_block) + rank;
   return true;
 }
@@ -88,8 +100,7 @@ __global__ __launch_bounds__(256) void k_store_rows_q8(RowsQ8Args a) {
     for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, w[j] & 0x7fff7fffu));
   }
   uint32_t A = max((uint32_t)top[0], (uint32_t)top[1]);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) A = max(A, (uint32_t)__shfl_xor((int)A, d));
+  A = wave_max(A);
   // A block with a value that is not finite has a NaN for its scale.
   float s = A >= 0x7f80u ? __builtin_nanf("") : fmaxf(__uint_as_float(A << 16), kQ8Least) / Q8<kFmt>::kMax;
   if (keep > 0 && !(s_old <= s)) s = s == s ? s_old : s;
