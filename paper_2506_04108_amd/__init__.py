@@ -484,13 +484,17 @@ class KVCacheQ8:
 
     def desc_q8(self) -> KVCacheQ8Desc:
         """The library's description of this cache. Its tensors are checked once
-        and again after one was replaced or moved (checking them took 8 us a call)."""
+        and again after one was replaced, moved or reshaped (checking them took 8 us
+        a call)."""
+        table = self.block_table
         where = (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
-                 self.kmin.data_ptr(), self.kmax.data_ptr())
+                 self.kmin.data_ptr(), self.kmax.data_ptr(), self.k.shape, self.v.shape, self.k_scale.shape,
+                 self.v_scale.shape, self.kmin.shape, self.kmax.shape,
+                 None if table is None else (table.data_ptr(), table.shape))
         checked = self._checked
         if checked is not None and checked[0] == where:
             return checked[1]
-        k, b, table = self.k, self.block_size, self.block_table
+        k, b = self.k, self.block_size
         fmt = _Q8_FORMATS.get(k.dtype)
         if fmt is None:
             raise TypeError(f"k must be torch.int8 or torch.float8_e4m3fn, got {k.dtype}")
