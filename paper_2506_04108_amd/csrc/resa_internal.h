@@ -208,7 +208,6 @@ int32_t select_blocks_per_wg(int32_t batch, int32_t kv_heads, int32_t max_blocks
 int32_t select_hist_words(int32_t batch, int32_t kv_heads, int32_t max_blocks_seq);
 int32_t decode_auto_splits(int32_t batch, int32_t kv_heads, int32_t n_cap, int32_t block_size);
 int32_t decode_q8_auto_splits(int32_t batch, int32_t kv_heads, int32_t n_cap, int32_t block_size);
-int32_t rows_waves(int32_t batch, int32_t rows, int32_t group);
 int32_t rows_chunk(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len);
 int32_t rows_max_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len);
 int32_t rectify_num_qblocks(int32_t group, int32_t f);

@@ -77,6 +77,16 @@ constexpr int kPacked = -1;                // source of keys: packed bf16 rows, 
 // (4 aligned rows, four neighbouring pieces) free of bank conflicts.
 __host__ __device__ constexpr int swz(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
 
+// Rows of a workgroup (64, 128 or 256) and its waves.
+__host__ __device__ constexpr int waves_of(int rows) { return rows == 256 ? 8 : 4; }
+// Over a cache: as few as hold a sequence's rows. 32 rows of one head for each
+// of 8 kv heads behind 8 x 32K: 183 us by 128 rows, 146 by 64; 32 rows of four
+// behind 8 x 64K 381 and 505.
+int rows_of_block(int32_t batch, int32_t rows, int32_t group) {
+  const int64_t all = (int64_t)rows * group;
+  return all <= (int64_t)64 * batch ? 64 : all <= (int64_t)128 * batch ? 128 : 256;
+}
+
 constexpr int kWaitVm0 = kWaitVmcnt0;
 
 // 1 or 2 KB of codes likewise.
@@ -212,32 +222,41 @@ struct RowsLds<kStages, true> {
   uint8_t raw[2][kKT * kHeadDim];
 };
 
-// With four stages of K and V (packed rows) one workgroup fits a CU, with two
-// stages and four waves two do. A barrier every kBar tiles, half the stages.
-template <int kWaves, int kStages, int kSrc, bool kPaged>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_rows_attn(RowsArgs a) {
+// A workgroup of kRows rows: 256 and 128 in 8 and 4 waves; 64 in 4 waves, of
+// which two share 32 rows, each with its half of every tile's keys, and are
+// merged at the end (few rows: a tile takes a wave half as long). With four
+// stages of K and V one workgroup fits a CU, with two stages and four waves two
+// do. A barrier every kBar tiles, half the stages.
+template <int kRows, int kSrc, bool kPaged>
+__global__ __launch_bounds__(kRows == 256 ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void k_rows_attn(RowsArgs a) {
   constexpr bool kQ8 = kSrc != kPacked;
+  constexpr int kWaves = waves_of(kRows);
+  constexpr bool kHalves = kRows == 64;
+  // Keys of a tile that a wave takes, in 32s and 16s.
+  constexpr int kMine32 = kHalves ? kKT32 / 2 : kKT32, kMine16 = 2 * kMine32;
+  constexpr int kStages = kRows == 256 && !kQ8 ? 4 : 2;
   // Weights and V: bf16, or over codes fp16.
   typedef std::conditional_t<kQ8, f16x8_t, bf16x8_t> P8;
   constexpr int kBar = kStages / 2;
   constexpr int kLoadRows = kKT / kWaves;  // tile rows whose K and V each wave brings in
   constexpr int kUnits = kLoadRows / 8;
-  constexpr int kRowsPerWg = kRowsPerWave * kWaves;
   constexpr int kTileBytes = kKT * kRowBytes;
   typedef RowsLds<kStages, kQ8> Lds;
   __shared__ __attribute__((aligned(1024))) Lds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rwave = kHalves ? wave & 1 : wave, half = kHalves ? wave >> 1 : 0;
   const int S = a.num_splits, G = a.group;
   const int hk = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % S;
   int seq, qblk;
   SeqRows sr;
-  if (!find_block<kSrc, kRowsPerWg>(a, rest / S, sr, seq, qblk)) return;
+  if (!find_block<kSrc, kRows>(a, rest / S, sr, seq, qblk)) return;
   if constexpr (!kQ8) {
     if (tid == 0) lds.odd = 0;
   }
   const int R = sr.n * G, past = sr.L - sr.n;
   const int k0 = split * a.chunk;
-  const int last_row = min(R - 1, (qblk + 1) * kRowsPerWg - 1);
+  const int last_row = min(R - 1, (qblk + 1) * kRows - 1);
   const int k1 = min(min(k0 + a.chunk, sr.L), past + last_row / G + 1);
   if (k1 <= k0) return;  // no key of this split is seen: the merge does not read it
   const int ntiles = (k1 - k0 + kKT - 1) / kKT;
@@ -246,7 +265,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const float c = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
   const uint32_t q_and = a.scale_log2 == 0.f ? 0u : ~0u, q_xor = a.scale_log2 < 0.f ? 0x80008000u : 0u;
   const int hi = lane >> 5, lq = lane & 31;
-  const int row_base = qblk * kRowsPerWg + wave * kRowsPerWave;
+  const int row_base = qblk * kRows + rwave * kRowsPerWave;
   const int rho = row_base + lq;
   // Keys past lim are masked. Rows past the last one follow it (their queries
   // are zero and nothing of theirs is stored).
@@ -254,7 +273,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   // Tiles that reach past `cut` (of the wave) or `wg_cut` (of any wave) mask
   // something.
   const int cut = min(k1, past + min(row_base, R - 1) / G);
-  const int wg_cut = past + qblk * kRowsPerWg / G;
+  const int wg_cut = past + qblk * kRows / G;
 
   // Packed rows straight into LDS: lane i fills slot i % 16 of rows i / 16 and
   // + 4 of each eight, fetching the row's piece (i % 16) ^ swz(row).
@@ -277,20 +296,20 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   // the slots differ in bit 1. The pieces of k-step ks and of dims 32 dt are an
   // exclusive or with 32 ks and 64 dt, taken once a round: held in registers
   // they make the kernels spill.
-  uint32_t kbase = lds0 + lq * kRowBytes + 16 * (hi ^ swz(lq));
+  uint32_t kbase = lds0 + (32 * half + lq) * kRowBytes + 16 * (hi ^ swz(lq));
   uint32_t vbase;
   {
     const int vr = 4 * hi + ((lane & 15) >> 2);
     const int vpiece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    vbase = lds0 + (uint32_t)offsetof(Lds, v) + vr * kRowBytes + 16 * (vpiece ^ swz(vr)) + 8 * (lane & 1);
+    vbase = lds0 + (uint32_t)offsetof(Lds, v) + (32 * half + vr) * kRowBytes + 16 * (vpiece ^ swz(vr)) + 8 * (lane & 1);
   }
   auto fresh = [](uint32_t& x) __attribute__((always_inline)) { __asm__ volatile("" : "+v"(x)); };
   typedef __attribute__((address_space(3))) const bf16x8_t lds_bf16x8;
   typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
   typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4;
-  auto read_k = [&](int st, int ks, bf16x8_t (&ka)[kKT32]) __attribute__((always_inline)) {
+  auto read_k = [&](int st, int ks, bf16x8_t (&ka)[kMine32]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kt = 0; kt < kKT32; ++kt)
+    for (int kt = 0; kt < kMine32; ++kt)
       ka[kt] = *(lds_bf16x8*)(uintptr_t)((kbase ^ (32 * ks)) + st * kTileBytes + kt * 32 * kRowBytes);
   };
   auto read_v32 = [&](int st, int ks, int dt) __attribute__((always_inline)) -> P8 {
@@ -316,11 +335,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const int qrow = lane >> 3;
   {
     // Row rel of the block's: a quotient of small numbers, exact in fp32.
-    const int r0 = (qblk * kRowsPerWg) / G, h0 = qblk * kRowsPerWg - r0 * G;
+    const int r0 = (qblk * kRows) / G, h0 = qblk * kRows - r0 * G;
     const float inv_g = 1.f / (float)G;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int rel = wave * kRowsPerWave + 8 * j + qrow + h0;
+      const int rel = rwave * kRowsPerWave + 8 * j + qrow + h0;
       const int dr = (int)(((float)rel + 0.5f) * inv_g);
       const uint16_t* qp = a.q + (int64_t)(sr.first + min(r0 + dr, sr.n - 1)) * a.q_stride +
                            (hk * G + rel - dr * G) * kHeadDim + 8 * (lane & 7);
@@ -466,16 +485,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     return w;
   };
   // Word w (0 .. 4 kUnits - 1) of them converted; every second one stores eight
-  // values to stage st (half: the four before).
-  auto put_word = [&](bool key, const Codes& c8, int w, int st, uint32_t (&half)[2]) __attribute__((always_inline)) {
+  // values to stage st (four: those before).
+  auto put_word = [&](bool key, const Codes& c8, int w, int st, uint32_t (&four)[2]) __attribute__((always_inline)) {
     uint32_t h[2];
     convert(key, c8.x[w / 4][w % 4], h);
     if (w % 2 == 0) {
-      half[0] = h[0];
-      half[1] = h[1];
+      four[0] = h[0];
+      four[1] = h[1];
     } else {
       uint8_t* tile = key ? lds.k[st] : lds.v[st];
-      st16(tile + 8 * (w / 4) * kRowBytes + ((w % 4 == 1 ? put0 : put1) ^ (32 * (w / 4))), U4{half[0], half[1], h[0], h[1]});
+      st16(tile + 8 * (w / 4) * kRowBytes + ((w % 4 == 1 ? put0 : put1) ^ (32 * (w / 4))), U4{four[0], four[1], h[0], h[1]});
     }
   };
   // Rows of tile ti of an odd block: NaN keys, zero values.
@@ -496,9 +515,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     if constexpr (kQ8) {
       compiler_fence();
       const Codes w = codes_at(from);
-      uint32_t half[2];
+      uint32_t four[2];
 #pragma unroll
-      for (int i = 0; i < 4 * kUnits; ++i) put_word(key, w, i, st, half);
+      for (int i = 0; i < 4 * kUnits; ++i) put_word(key, w, i, st, four);
       put_odd(key, ti, st);
       compiler_fence();  // the codes have been read when the next are asked for
     }
@@ -515,22 +534,22 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   float m = ninf, l = 0.f;  // l: over this lane's keys; summed across the two halves at the end
   bool guard = false;       // second pass, V values that are not finite left out
 
-  auto mask = [&](int t0, f32x16_t (&s)[kKT32]) __attribute__((always_inline)) {
-    const int d = lim - t0 - 4 * hi;
+  auto mask = [&](int t0, f32x16_t (&s)[kMine32]) __attribute__((always_inline)) {
+    const int d = lim - t0 - 32 * half - 4 * hi;
 #pragma unroll
-    for (int kt = 0; kt < kKT32; ++kt)
+    for (int kt = 0; kt < kMine32; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[kt][i] = 32 * kt + 8 * (i >> 2) + (i & 3) > d ? ninf : s[kt][i];
   };
   // Factors of a tile's scores and of its weights, for each 16 keys. Those of
   // the scores are read with the K they belong to, a round before their use.
   struct Factors {
-    float x[kKT16];
+    float x[kMine16];
   };
   auto key_factors = [&](int ti) __attribute__((always_inline)) -> Factors {
     Factors f;
 #pragma unroll
-    for (int i = 0; i < kKT16; ++i) f.x[i] = kQ8 ? lane_f(win.kf, block_at(ti * kKT + 16 * i)) : c;
+    for (int i = 0; i < kMine16; ++i) f.x[i] = kQ8 ? lane_f(win.kf, block_at(ti * kKT + 32 * half + 16 * i)) : c;
     return f;
   };
   // fp16 weights carry the value scale over vref, a power of two above the
@@ -554,19 +573,19 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       }
       const float inv = __uint_as_float(0x7f000000u - vref);  // 1 / vref
 #pragma unroll
-      for (int i = 0; i < kKT16; ++i) f.x[i] = __uint_as_float(x[i]) * inv;
+      for (int i = 0; i < kMine16; ++i) f.x[i] = __uint_as_float(half != 0 ? x[i + kKT16 - kMine16] : x[i]) * inv;
     }
     return f;
   };
-  auto row_max = [&](const f32x16_t (&s)[kKT32], const Factors& f) __attribute__((always_inline)) {
+  auto row_max = [&](const f32x16_t (&s)[kMine32], const Factors& f) __attribute__((always_inline)) {
     float x = ninf;
 #pragma unroll
-    for (int kt = 0; kt < kKT32; ++kt)
+    for (int kt = 0; kt < kMine32; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) x = fmaxf(x, s[kt][i] * f.x[2 * kt + (i >> 3)]);
     return max_xor32(x);
   };
-  auto weight = [&](float y, int i, const Factors& g, P8 (&ph)[kKT16], float (&ps)[4]) __attribute__((always_inline)) {
+  auto weight = [&](float y, int i, const Factors& g, P8 (&ph)[kMine16], float (&ps)[4]) __attribute__((always_inline)) {
     const float pe = fast_exp2(y);
     ps[i & 3] = i < 4 ? pe : ps[i & 3] + pe;
     if constexpr (kQ8)
@@ -574,29 +593,29 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     else
       ph[i >> 3][i & 7] = (__bf16)pe;
   };
-  auto scores = [&](int st, f32x16_t (&s)[kKT32]) __attribute__((always_inline)) {
-    bf16x8_t ka[kKT32];
+  auto scores = [&](int st, f32x16_t (&s)[kMine32]) __attribute__((always_inline)) {
+    bf16x8_t ka[kMine32];
 #pragma unroll
-    for (int kt = 0; kt < kKT32; ++kt)
+    for (int kt = 0; kt < kMine32; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
       read_k(st, ks, ka);
 #pragma unroll
-      for (int kt = 0; kt < kKT32; ++kt) s[kt] = mfma32(ka[kt], qb[ks], s[kt]);
+      for (int kt = 0; kt < kMine32; ++kt) s[kt] = mfma32(ka[kt], qb[ks], s[kt]);
     }
   };
   // Weights of one tile (scores s) interleaved with the scores of the next
   // (K stage st, into sn).
-  auto weights_scores = [&](auto stage, const f32x16_t (&s)[kKT32], f32x16_t (&sn)[kKT32], const Factors& f,
-                            const Factors& g, P8 (&ph)[kKT16]) __attribute__((always_inline)) {
+  auto weights_scores = [&](auto stage, const f32x16_t (&s)[kMine32], f32x16_t (&sn)[kMine32], const Factors& f,
+                            const Factors& g, P8 (&ph)[kMine16]) __attribute__((always_inline)) {
     constexpr int st = decltype(stage)::value;
     float ps[4] = {0.f, 0.f, 0.f, 0.f};
-    bf16x8_t ka[2][kKT32];
+    bf16x8_t ka[2][kMine32];
     read_k(st, 0, ka[0]);
 #pragma unroll
-    for (int kt = 0; kt < kKT32; ++kt)
+    for (int kt = 0; kt < kMine32; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sn[kt][i] = 0.f;
     __builtin_amdgcn_sched_barrier(0);
@@ -605,10 +624,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int ks = 0; ks < 8; ++ks) {
       if (ks < 7) read_k(st, ks + 1, ka[(ks + 1) & 1]);
 #pragma unroll
-      for (int kt = 0; kt < kKT32; ++kt) {
+      for (int kt = 0; kt < kMine32; ++kt) {
         sn[kt] = mfma32(ka[ks & 1][kt], qb[ks], sn[kt]);
 #pragma unroll
-        for (int i = 2 * (kKT32 * ks + kt); i < 2 * (kKT32 * ks + kt) + 2; ++i)
+        for (int i = 2 * (kMine32 * ks + kt); i < 2 * (kMine32 * ks + kt) + 2; ++i)
           weight(fmaf(s[i >> 4][i & 15], f.x[i >> 3], -m), i, g, ph, ps);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -625,7 +644,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   // K(p + kBar + 1) .. K(p + 2 kBar) and V(p + kBar) .. V(p + 2 kBar - 1) are
   // brought into them, and are there at the next barrier, before which every
   // wave has waited for its own.
-  auto round = [&](int ti, auto stage, f32x16_t (&s)[kKT32], f32x16_t (&sn)[kKT32], const Factors& f,
+  auto round = [&](int ti, auto stage, f32x16_t (&s)[kMine32], f32x16_t (&sn)[kMine32], const Factors& f,
                    Factors& fn) __attribute__((always_inline)) {
     constexpr int st = decltype(stage)::value;
     const int t0 = k0 + ti * kKT;
@@ -669,7 +688,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
     const Factors g = value_factors(ti);
     fn = key_factors(ti + 1);
-    P8 ph[kKT16];
+    P8 ph[kMine16];
     fresh(kbase);
     __builtin_amdgcn_sched_barrier(0);
     float ps = weights_scores(std::integral_constant<int, (st + 1) % kStages>{}, s, sn, f, g, ph);
@@ -687,7 +706,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       // From the rounded logits that the reference is the maximum of: with
       // logits past 2^31 the unrounded product may exceed it by hundreds.
 #pragma unroll
-      for (int i = 0; i < 16 * kKT32; ++i) weight(sub_rounded(s[i >> 4][i & 15] * f.x[i >> 3], mref), i, g, ph, pt);
+      for (int i = 0; i < 16 * kMine32; ++i) weight(sub_rounded(s[i >> 4][i & 15] * f.x[i >> 3], mref), i, g, ph, pt);
       ps = (pt[0] + pt[1]) + (pt[2] + pt[3]);
     }
     l += ps;
@@ -702,22 +721,24 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
     __builtin_amdgcn_sched_barrier(0);
     P8 va[2][4];
-    uint32_t half[2];
+    uint32_t four[2];
     fresh(vbase);
     read_v(st, 0, va[0]);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int ks = 0; ks < kKT16; ++ks) {
-      if (ks < kKT16 - 1) read_v(st, ks + 1, va[(ks + 1) & 1]);
+    for (int ks = 0; ks < kMine16; ++ks) {
+      if (ks < kMine16 - 1) read_v(st, ks + 1, va[(ks + 1) & 1]);
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt) {
         o[dt] = mfma32(va[ks & 1][dt], ph[ks], o[dt]);
-        // A word of codes under every MFMA (8 waves: under every second).
+        // The words of codes (K's, then V's) shared out under the MFMAs.
         if constexpr (kQ8) {
-          const int n = 4 * ks + dt, w = n * kUnits / 2;
-          if (kUnits == 2 || n % 2 == 1) {
-            if (w < 4 * kUnits) put_word(true, wk, w, st, half);
-            else put_word(false, wv, w - 4 * kUnits, (st + 1) % kStages, half);
+          constexpr int kWords = 8 * kUnits, kMfmas = 4 * kMine16;
+          const int n = 4 * ks + dt;
+#pragma unroll
+          for (int w = n * kWords / kMfmas; w < (n + 1) * kWords / kMfmas; ++w) {
+            if (w < 4 * kUnits) put_word(true, wk, w, st, four);
+            else put_word(false, wv, w - 4 * kUnits, (st + 1) % kStages, four);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -769,7 +790,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     bare_barrier();
-    f32x16_t sa[kKT32], sb[kKT32];
+    f32x16_t sa[kMine32], sb[kMine32];
     scores(0, sa);
     if (k0 + kKT > cut) mask(k0, sa);
     Factors fa = key_factors(0), fb;
@@ -798,6 +819,36 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     clear_o();
     l = 0.f;
     request();
+  }
+
+  // The halves of the keys: the second waves hand over what they have.
+  if constexpr (kHalves) {
+    f32x4_t* slot = reinterpret_cast<f32x4_t*>(lds.k[0]) + rwave * (17 * 64) + lane;
+    static_assert(2 * 17 * 64 * sizeof(f32x4_t) <= sizeof(Lds::k) + sizeof(Lds::v));
+    if (half == 1) {
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4)
+          slot[64 * (4 * dt + i4)] = f32x4_t{o[dt][4 * i4], o[dt][4 * i4 + 1], o[dt][4 * i4 + 2], o[dt][4 * i4 + 3]};
+      slot[64 * 16] = f32x4_t{m, l, 0.f, 0.f};
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    bare_barrier();
+    if (half == 1) return;
+    const f32x4_t ml = slot[64 * 16];
+    const float mn = fmaxf(m, ml[0]);
+    const float x0 = m == mn ? 1.f : fast_exp2(m - mn), x1 = ml[0] == mn ? 1.f : fast_exp2(ml[0] - mn);
+    m = mn;
+    l = l * x0 + ml[1] * x1;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const f32x4_t p = slot[64 * (4 * dt + i4)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) o[dt][4 * i4 + u] = o[dt][4 * i4 + u] * x0 + p[u] * x1;
+      }
   }
 
   // V values that are not finite, cleared in the second pass: whoever sees
@@ -923,26 +974,22 @@ __global__ __launch_bounds__(256) void k_rows_combine(RowsArgs a) {
 }
 
 // Query blocks of a launch at most: a sequence's last one may not be full.
-int64_t most_blocks(const RowsArgs& a, int waves) {
-  return (int64_t)a.rows * a.group / (kRowsPerWave * waves) + a.batch;
-}
+int64_t most_blocks(const RowsArgs& a, int per) { return (int64_t)a.rows * a.group / per + a.batch; }
 
-template <int kWaves, int kStages, int kSrc, bool kPaged>
+template <int kRows, int kSrc, bool kPaged>
 hipError_t launch_attn(const RowsArgs& a, hipStream_t stream) {
-  const int64_t grid = most_blocks(a, kWaves) * a.num_splits * a.kv_heads;
+  const int64_t grid = most_blocks(a, kRows) * a.num_splits * a.kv_heads;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_rows_attn<kWaves, kStages, kSrc, kPaged>), dim3((uint32_t)grid), dim3(64 * kWaves), 0, stream, a);
+  hipLaunchKernelGGL((k_rows_attn<kRows, kSrc, kPaged>), dim3((uint32_t)grid), dim3(64 * waves_of(kRows)), 0, stream, a);
   return hipGetLastError();
 }
 
-template <int kSrc>
+template <int kSrc, bool kPaged>
 hipError_t launch_q8(const RowsArgs& a, hipStream_t stream) {
-  const bool paged = a.c.table != nullptr;
-  hipError_t e;
-  if (rows_waves(a.batch, a.rows, a.group) == 4)
-    e = paged ? launch_attn<4, 2, kSrc, true>(a, stream) : launch_attn<4, 2, kSrc, false>(a, stream);
-  else
-    e = paged ? launch_attn<8, 2, kSrc, true>(a, stream) : launch_attn<8, 2, kSrc, false>(a, stream);
+  const int rows = rows_of_block(a.batch, a.rows, a.group);
+  const hipError_t e = rows == 64    ? launch_attn<64, kSrc, kPaged>(a, stream)
+                       : rows == 128 ? launch_attn<128, kSrc, kPaged>(a, stream)
+                                     : launch_attn<256, kSrc, kPaged>(a, stream);
   if (e != hipSuccess || a.num_splits == 1) return e;
   const int64_t outs = (int64_t)a.rows * a.q_heads;
   hipLaunchKernelGGL(k_rows_combine<kSrc>, dim3((uint32_t)((outs + 3) / 4)), dim3(256), 0, stream, a);
@@ -951,22 +998,16 @@ hipError_t launch_q8(const RowsArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-// Waves of a workgroup: four (128 rows) where a sequence's rows are no more.
-int32_t rows_waves(int32_t batch, int32_t rows, int32_t group) {
-  return (int64_t)rows * group <= (int64_t)128 * batch ? 4 : 8;
-}
-
 // Key splits at most: enough for a workgroup on every CU, and for a second one
 // (of 4 waves) where a split stays long: every split writes its rows' sums and
 // the merge reads them again. 32 rows of 32 heads behind 8K: 32.9 us with one
 // workgroup a CU, 40.0 with two; behind 8 x 64K 444 and 384.
 static int64_t rows_most_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
-  const int waves = rows_waves(batch, rows, group);
-  const int64_t per = kRowsPerWave * waves;
+  const int per = rows_of_block(batch, rows, group);
   const int64_t each = ((int64_t)((rows + batch - 1) / batch) * group + per - 1) / per;
   const int64_t wgs = (each < 1 ? 1 : each) * batch * kv_heads;
   const auto splits = [&](int64_t want) { return wgs >= want ? 1 : (want + wgs - 1) / wgs; };
-  return waves == 4 && max_seq_len >= kLongSplit * splits(kCus) ? splits(2 * kCus) : splits(kCus);
+  return per < 256 && max_seq_len >= kLongSplit * splits(kCus) ? splits(2 * kCus) : splits(kCus);
 }
 
 int32_t rows_chunk(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
@@ -984,13 +1025,18 @@ int32_t rows_max_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t 
 }
 
 hipError_t launch_rows_q8(const RowsArgs& a, int32_t format, hipStream_t stream) {
-  return format == RESA_Q8_INT8 ? launch_q8<RESA_Q8_INT8>(a, stream) : launch_q8<RESA_Q8_E4M3>(a, stream);
+  const bool paged = a.c.table != nullptr;
+  if (format == RESA_Q8_INT8) return paged ? launch_q8<RESA_Q8_INT8, true>(a, stream) : launch_q8<RESA_Q8_INT8, false>(a, stream);
+  return paged ? launch_q8<RESA_Q8_E4M3, true>(a, stream) : launch_q8<RESA_Q8_E4M3, false>(a, stream);
 }
 
 hipError_t launch_prompt(const RowsArgs& a, hipStream_t stream) {
-  // Small launches in 4-wave workgroups, two a CU.
-  return most_blocks(a, 8) * a.kv_heads < 2 * kCus ? launch_attn<4, 2, kPacked, false>(a, stream)
-                                                   : launch_attn<8, 4, kPacked, false>(a, stream);
+  // Small launches in small workgroups, as long as all of them run at once (two
+  // a CU): 1000 tokens of 32 / 8 heads 27.3 us by 128 rows, 24.5 by 64; 8 prompts
+  // of up to 250, whose 625 blocks do not, 15.3 and 19.6.
+  if (most_blocks(a, 64) * a.kv_heads <= 2 * kCus) return launch_attn<64, kPacked, false>(a, stream);
+  return most_blocks(a, 256) * a.kv_heads < 2 * kCus ? launch_attn<128, kPacked, false>(a, stream)
+                                                     : launch_attn<256, kPacked, false>(a, stream);
 }
 
 }  // namespace resa
