@@ -562,10 +562,11 @@ def _one_device(first: torch.Tensor, *others) -> None:
             raise ValueError(f"tensors are on devices {index} and {t.get_device()}")
 
 
-def _new(stream, device, *wanted):
-    """New tensors ((shape, dtype), ...) that belong to the stream a call runs on."""
+def _new(stream, like: torch.Tensor, *wanted):
+    """New tensors ((shape, dtype), ...) on like's device that belong to the
+    stream a call runs on."""
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-        return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
+        return [like.new_empty(shape, dtype=dtype, requires_grad=False) for shape, dtype in wanted]
 
 
 def _with_workspace(call, needs, workspace, stream, device):
@@ -600,9 +601,9 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     if sm_scale is None:
         sm_scale = _SCALE
     if out is None:
-        out, = _new(stream, q.device, ((T, hq, HEAD_DIM), torch.bfloat16))
+        out, = _new(stream, q, ((T, hq, HEAD_DIM), torch.bfloat16))
     if lse is None and with_lse:
-        lse, = _new(stream, q.device, ((T, hq), torch.float32))
+        lse, = _new(stream, q, ((T, hq), torch.float32))
     _need(out, "out", torch.bfloat16, (T, hq, HEAD_DIM))
     if lse is not None:
         _need(lse, "lse", torch.float32, (T, hq))
@@ -641,7 +642,7 @@ def load_rows_q8(cache: KVCacheQ8, cu_rows: torch.Tensor, seq_lens: torch.Tensor
     if out is None:
         if num_rows is None:
             raise ValueError("either num_rows or out must be given")
-        out = tuple(_new(stream, cache.k.device, *[((num_rows, H, HEAD_DIM), torch.bfloat16)] * 2))
+        out = tuple(_new(stream, cache.k, *[((num_rows, H, HEAD_DIM), torch.bfloat16)] * 2))
     k_rows, v_rows = out
     T = k_rows.shape[0]
     _need(k_rows, "k_rows", torch.bfloat16, (T, H, HEAD_DIM))
@@ -668,9 +669,9 @@ def sparse_decode_q8(cache: KVCacheQ8, q: torch.Tensor, seq_lens: torch.Tensor, 
     _need(block_idx, "block_idx", torch.int32, (B, H, n_cap))
     _need(num_sel, "num_sel", torch.int32, (B, H))
     if out is None:
-        out, = _new(stream, q.device, ((B, hq, HEAD_DIM), torch.float32))
+        out, = _new(stream, q, ((B, hq, HEAD_DIM), torch.float32))
     if lse is None and with_lse:
-        lse, = _new(stream, q.device, ((B, hq), torch.float32))
+        lse, = _new(stream, q, ((B, hq), torch.float32))
     _need(out, "out", torch.float32, (B, hq, HEAD_DIM))
     if lse is not None:
         _need(lse, "lse", torch.float32, (B, hq))
@@ -703,9 +704,9 @@ def dense_rectify_q8(cache: KVCacheQ8, q_rows: torch.Tensor, k_rows: torch.Tenso
     _need(cu_rows, "cu_rows", torch.int32, (B + 1,))
     _need(seq_lens, "seq_lens", torch.int32, (B,))
     if out is None:
-        out, = _new(stream, q_rows.device, ((T, hq, HEAD_DIM), torch.bfloat16))
+        out, = _new(stream, q_rows, ((T, hq, HEAD_DIM), torch.bfloat16))
     if lse is None and with_lse:
-        lse, = _new(stream, q_rows.device, ((T, hq), torch.float32))
+        lse, = _new(stream, q_rows, ((T, hq), torch.float32))
     _need(out, "out", torch.bfloat16, (T, hq, HEAD_DIM))
     if lse is not None:
         _need(lse, "lse", torch.float32, (T, hq))
