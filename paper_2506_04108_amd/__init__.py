@@ -483,17 +483,19 @@ class KVCacheQ8:
         object.__setattr__(self, "_checked", None)
 
     def desc_q8(self) -> KVCacheQ8Desc:
-        """The library's description of this cache. Its tensors are checked once
-        and again after one was replaced, moved or reshaped (checking them took 8 us
-        a call)."""
+        """The library's description of this cache."""
+        return self._described()[1]
+
+    def _described(self):
+        """(the cache's memory, its description, a reference to that, batch, kv
+        heads). The tensors are checked once, and again after one was replaced or
+        its memory moved (checking them took 8 us a call)."""
         table = self.block_table
         where = (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
-                 self.kmin.data_ptr(), self.kmax.data_ptr(), self.k.shape, self.v.shape, self.k_scale.shape,
-                 self.v_scale.shape, self.kmin.shape, self.kmax.shape,
-                 None if table is None else (table.data_ptr(), table.shape))
+                 self.kmin.data_ptr(), self.kmax.data_ptr(), None if table is None else table.data_ptr())
         checked = self._checked
         if checked is not None and checked[0] == where:
-            return checked[1]
+            return checked
         k, b = self.k, self.block_size
         fmt = _Q8_FORMATS.get(k.dtype)
         if fmt is None:
@@ -514,8 +516,9 @@ class KVCacheQ8:
         _one_device(k, self.v, self.k_scale, self.v_scale, self.kmin, self.kmax, table)
         d = KVCacheQ8Desc(KVCacheDesc(where[0], where[1], where[4], where[5], B, H, HEAD_DIM, mb * b, b, tp, pages),
                           where[2], where[3], fmt)
-        object.__setattr__(self, "_checked", (where, d))
-        return d
+        checked = (where, d, C.byref(d), B, H)
+        object.__setattr__(self, "_checked", checked)
+        return checked
 
 
 def _packed(t: torch.Tensor, name: str, rows: int, heads: int) -> int:
@@ -622,14 +625,14 @@ def store_rows_q8(cache: KVCacheQ8, k_rows: torch.Tensor, v_rows: torch.Tensor, 
     ``[cu_rows[s], cu_rows[s + 1])`` of k_rows, v_rows ``[T, Hkv, 128]`` (bf16)
     become the last positions of sequence s, whose ``seq_lens`` already counts
     them."""
-    d = cache.desc_q8()
-    B, H, T = d.base.batch, d.base.num_kv_heads, k_rows.shape[0]
+    _, _, ref, B, H = cache._described()
+    T = k_rows.shape[0]
     ks, vs = _packed(k_rows, "k_rows", T, H), _packed(v_rows, "v_rows", T, H)
     _need(cu_rows, "cu_rows", torch.int32, (B + 1,))
     _need(seq_lens, "seq_lens", torch.int32, (B,))
     _one_device(cache.k, k_rows, v_rows, cu_rows, seq_lens)
     if T:
-        check(lib().resa_store_rows_q8(C.byref(d), k_rows.data_ptr(), v_rows.data_ptr(), ks, vs, cu_rows.data_ptr(),
+        check(lib().resa_store_rows_q8(ref, k_rows.data_ptr(), v_rows.data_ptr(), ks, vs, cu_rows.data_ptr(),
                                        T, seq_lens.data_ptr(), _stream(stream)))
 
 
@@ -637,8 +640,7 @@ def load_rows_q8(cache: KVCacheQ8, cu_rows: torch.Tensor, seq_lens: torch.Tensor
                  out: tuple | None = None, stream=None):
     """The last rows of each sequence as bf16, ``(k_rows, v_rows)`` of ``[T,
     Hkv, 128]``: ``out``, or new tensors of ``num_rows`` rows."""
-    d = cache.desc_q8()
-    B, H = d.base.batch, d.base.num_kv_heads
+    _, _, ref, B, H = cache._described()
     if out is None:
         if num_rows is None:
             raise ValueError("either num_rows or out must be given")
@@ -651,7 +653,7 @@ def load_rows_q8(cache: KVCacheQ8, cu_rows: torch.Tensor, seq_lens: torch.Tensor
     _need(seq_lens, "seq_lens", torch.int32, (B,))
     _one_device(cache.k, k_rows, v_rows, cu_rows, seq_lens)
     if T:
-        check(lib().resa_load_rows_q8(C.byref(d), cu_rows.data_ptr(), T, seq_lens.data_ptr(), k_rows.data_ptr(),
+        check(lib().resa_load_rows_q8(ref, cu_rows.data_ptr(), T, seq_lens.data_ptr(), k_rows.data_ptr(),
                                       v_rows.data_ptr(), _stream(stream)))
     return k_rows, v_rows
 
@@ -662,8 +664,8 @@ def sparse_decode_q8(cache: KVCacheQ8, q: torch.Tensor, seq_lens: torch.Tensor, 
                      workspace: Workspace | None = None, stream=None):
     """:func:`sparse_decode` over an 8-bit cache. Returns ``(out fp32 [B, Hq,
     128], lse fp32 [B, Hq] or None)``."""
-    d = cache.desc_q8()
-    B, H, hq, n_cap = d.base.batch, d.base.num_kv_heads, q.shape[1], block_idx.shape[-1]
+    _, _, ref, B, H = cache._described()
+    hq, n_cap = q.shape[1], block_idx.shape[-1]
     _need(q, "q", torch.bfloat16, (B, hq, HEAD_DIM))
     _need(seq_lens, "seq_lens", torch.int32, (B,))
     _need(block_idx, "block_idx", torch.int32, (B, H, n_cap))
@@ -677,7 +679,7 @@ def sparse_decode_q8(cache: KVCacheQ8, q: torch.Tensor, seq_lens: torch.Tensor, 
         _need(lse, "lse", torch.float32, (B, hq))
     _one_device(cache.k, q, seq_lens, block_idx, num_sel, out, lse)
     scale = _SCALE if sm_scale is None else float(sm_scale)
-    ptrs = (C.byref(d), q.data_ptr(), hq, seq_lens.data_ptr(), block_idx.data_ptr(), num_sel.data_ptr(), n_cap,
+    ptrs = (ref, q.data_ptr(), hq, seq_lens.data_ptr(), block_idx.data_ptr(), num_sel.data_ptr(), n_cap,
             num_splits, scale, out.data_ptr(), _ptr(lse))
     run, st = lib().resa_sparse_decode_q8, _stream(stream)
     _with_workspace(lambda ws, size: run(*ptrs, ws, size, st),
@@ -697,8 +699,8 @@ def dense_rectify_q8(cache: KVCacheQ8, q_rows: torch.Tensor, k_rows: torch.Tenso
     ``max_seq_len`` bounds seq_lens. Returns ``(out bf16 [T, Hq, 128], lse fp32
     [T, Hq] or None)``; rows of sequences without rows in the call are not
     written."""
-    d = cache.desc_q8()
-    B, H, T, hq = d.base.batch, d.base.num_kv_heads, q_rows.shape[0], q_rows.shape[1]
+    _, _, ref, B, H = cache._described()
+    T, hq = q_rows.shape[0], q_rows.shape[1]
     qs = _packed(q_rows, "q_rows", T, hq)
     ks, vs = _packed(k_rows, "k_rows", T, H), _packed(v_rows, "v_rows", T, H)
     _need(cu_rows, "cu_rows", torch.int32, (B + 1,))
@@ -713,7 +715,7 @@ def dense_rectify_q8(cache: KVCacheQ8, q_rows: torch.Tensor, k_rows: torch.Tenso
     _one_device(cache.k, q_rows, k_rows, v_rows, cu_rows, seq_lens, out, lse)
     if T:
         scale = _SCALE if sm_scale is None else float(sm_scale)
-        ptrs = (C.byref(d), q_rows.data_ptr(), k_rows.data_ptr(), v_rows.data_ptr(), qs, ks, vs, hq,
+        ptrs = (ref, q_rows.data_ptr(), k_rows.data_ptr(), v_rows.data_ptr(), qs, ks, vs, hq,
                 cu_rows.data_ptr(), T, seq_lens.data_ptr(), max_seq_len, scale, out.data_ptr(), _ptr(lse))
         run, st = lib().resa_dense_rectify_q8, _stream(stream)
         _with_workspace(lambda ws, size: run(*ptrs, ws, size, st),
