@@ -27,7 +27,7 @@
 // weights of a tile sum to more than 2^12 over a lane's keys, so that no tile
 // needs its maximum beforehand.
 //
-// The query blocks are dealt longest first (every workgroup finds its own by
+// The query blocks are dealt long ones first (every workgroup finds its own by
 // a search over the sequences' counts, in one wave's registers), with the kv
 // heads of a block next to each other: workgroups go to the 8 XCDs in turn,
 // so that with 8 kv heads the blocks of one head share an L2.
@@ -44,7 +44,7 @@
 // cycles and the VALU 55 %).
 //
 // Measured: one prompt of 16384 tokens, 32 heads over 8: 1.86 ms, 1.18 PFLOP/s; 16
-// prompts of 77 to 2000 tokens, 28 heads over 4: 221 us, 0.76 PFLOP/s, of which a
+// prompts of 77 to 2000 tokens, 28 heads over 4: 214 us, 0.78 PFLOP/s, of which a
 // workgroup's start (its block, queries, first tiles) and end take 60; one of 300
 // tokens 10.2 us, a chain of latencies. 32 rows of 4 heads behind 8 x 64K codes:
 // 357 us with the stores and the merge, 3.0 TB/s; 2033 rows of 7 behind 31K:
@@ -74,6 +74,7 @@ constexpr int kKT = 64;                    // keys per tile
 constexpr int kKT32 = kKT / 32, kKT16 = kKT / 16;
 constexpr int kRowBytes = kHeadDim * 2;
 constexpr int kCus = 256;
+constexpr int kClassKeys = 1024;          // query blocks: a class of costs
 constexpr int64_t kLongSplit = 1024;      // keys of a split that is long
 constexpr float kMaxWeightSum = 4096.f;
 constexpr int kPacked = -1;                // source of keys: packed bf16 rows, else the format of the 8-bit cache
@@ -147,15 +148,20 @@ __device__ __forceinline__ SeqRows seq_rows(const RowsArgs& a, int s) {
   return q;
 }
 
-// Query block `item`, longest first. A block's cost is its last row's position
-// in units of a block's rows: block b of a sequence with h rows' worth of
-// earlier keys costs h + b + 1. The cost of item i is the largest x with more
-// than i blocks of cost >= x; among the blocks of that cost the sequences come
-// in order. The first 64 sequences' counts stay in registers, so that up to
-// there the search reads memory once.
+// Query block `item`, the longest first. A block's cost is its last row's
+// position in units of a block's rows: block b of a sequence with h rows' worth
+// of earlier keys costs h + b + 1. The blocks are dealt by classes of cost, of
+// kClassKeys keys each, from the highest down, those of a class sequence by
+// sequence: workgroups that run together then share the keys of a sequence, in
+// the L2, and the last ones are short all the same. Against strictly falling
+// costs: 16 prompts of up to 2000 tokens, 28 heads over 4, 224 -> 214 us; 64 of up to
+// 700, 32 over 8, 233 -> 202; 30 of 1000, 8 over 8, whose last class is a larger part of
+// the whole, 63.5 -> 67.8. (Blocks of different costs next to each other: 16 prompts 259
+// and more.) The first 64 sequences' counts stay in registers, so that up to there the search reads memory once.
 template <int kSrc, int kPer>
 __device__ __forceinline__ bool find_block(const RowsArgs& a, int item, SeqRows& sr, int& seq, int& qblk) {
   const int lane = threadIdx.x & 63;
+  const int per = max(kClassKeys * a.group / kPer, 1);  // costs of a class: x per + 1 .. (x + 1) per
   auto earlier = [&](const SeqRows& q) -> int {
     return kSrc == kPacked ? 0 : (int)((int64_t)(q.L - q.n) * a.group / kPer);
   };
@@ -163,51 +169,51 @@ __device__ __forceinline__ bool find_block(const RowsArgs& a, int item, SeqRows&
   auto rows_at = [&](int s) -> SeqRows { return s < a.batch ? seq_rows<kSrc>(a, s) : SeqRows{0, 0, 0}; };
   const SeqRows q0 = rows_at(lane);
   const int h0 = earlier(q0), nb0 = blocks(q0);
-  int lo, rank = 0;
+  int x = 0, rank = item;
   seq = 0;
   if (a.batch == 1) {
-    const int h = __builtin_amdgcn_readlane(h0, 0), nb = __builtin_amdgcn_readlane(nb0, 0);
-    if (nb <= item) return false;
-    lo = h + nb - item;
+    if (__builtin_amdgcn_readlane(nb0, 0) <= item) return false;
   } else {
-    auto at_least = [&](int x) -> int {  // blocks of cost >= x
-      int c = min(max(h0 + nb0 - x + 1, 0), nb0);
+    auto of = [&](int h, int nb, int x) -> int { return min(max(h + nb - x * per, 0), nb); };
+    auto at_least = [&](int x) -> int {  // blocks of class x and above
+      int c = of(h0, nb0, x);
       for (int base = 64; base < a.batch; base += 64) {
         const SeqRows q = rows_at(base + lane);
-        const int nb = blocks(q);
-        c += min(max(earlier(q) + nb - x + 1, 0), nb);
+        c += of(earlier(q), blocks(q), x);
       }
       return wave_total(c);
     };
-    int most = nb0 == 0 ? 0 : h0 + nb0, least = nb0 == 0 ? INT32_MAX : h0 + 1;
+    int most = nb0 == 0 ? 0 : h0 + nb0, least = nb0 == 0 ? INT32_MAX : h0;
     for (int base = 64; base < a.batch; base += 64) {
       const SeqRows q = rows_at(base + lane);
       const int h = earlier(q), nb = blocks(q);
       if (nb > 0) {
         most = max(most, h + nb);
-        least = min(least, h + 1);
+        least = min(least, h);
       }
     }
     most = (int)wave_max((uint32_t)most);
-    lo = (int)~wave_max(~(uint32_t)least);
-    if (at_least(1) <= item) return false;
-    int hi = most + 1;  // more than `item` blocks of cost >= lo, not of cost >= hi
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (at_least(mid) > item) lo = mid;
+    if (most == 0) return false;
+    x = (int)~wave_max(~(uint32_t)least) / per;
+    if (at_least(x) <= item) return false;
+    int hi = (most - 1) / per + 1;  // more than `item` blocks of class x and above, not of class hi
+    while (hi - x > 1) {
+      const int mid = (x + hi) >> 1;
+      if (at_least(mid) > item) x = mid;
       else hi = mid;
     }
-    auto of_cost = [&](int s) -> int {
+    auto of_class = [&](int s) -> int {
       const SeqRows q = s < 64 ? q0 : rows_at(s);
-      const int h = earlier(q);
-      return lo > h && lo <= h + blocks(q) ? 1 : 0;
+      const int h = earlier(q), nb = blocks(q);
+      return of(h, nb, x) - of(h, nb, x + 1);
     };
-    if (!find_seq(item - at_least(lo + 1), a.batch, of_cost, seq, rank)) return false;
+    if (!find_seq(item - at_least(x + 1), a.batch, of_class, seq, rank)) return false;
   }
   sr = seq < 64 ? SeqRows{__builtin_amdgcn_readlane(q0.first, seq & 63), __builtin_amdgcn_readlane(q0.n, seq & 63),
                           __builtin_amdgcn_readlane(q0.L, seq & 63)}
                 : seq_rows<kSrc>(a, seq);
-  qblk = lo - earlier(sr) - 1;
+  const int h = earlier(sr), last = h + blocks(sr);
+  qblk = (a.batch == 1 ? last : min(last, (x + 1) * per)) - rank - h - 1;
   return true;
 }
 
