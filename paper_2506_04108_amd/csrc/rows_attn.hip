@@ -48,7 +48,7 @@
 // workgroup's start (its block, queries, first tiles) and end take 60; one of 300
 // tokens 10.2 us, a chain of latencies. 32 rows of 4 heads behind 8 x 64K codes:
 // 357 us with the stores and the merge, 3.0 TB/s; 2033 rows of 7 behind 31K:
-// 1.46 ms, 0.95 PFLOP/s.
+// 1.39 ms, 0.99 PFLOP/s.
 //
 // Masked keys: scores are replaced, so nothing of a masked K row matters; a
 // masked V row meets weights of zero, which only a value that is not finite
@@ -157,7 +157,8 @@ __device__ __forceinline__ SeqRows seq_rows(const RowsArgs& a, int s) {
 // costs: 16 prompts of up to 2000 tokens, 28 heads over 4, 224 -> 214 us; 64 of up to
 // 700, 32 over 8, 233 -> 202; 30 of 1000, 8 over 8, whose last class is a larger part of
 // the whole, 63.5 -> 67.8. (Blocks of different costs next to each other: 16 prompts 259
-// and more.) The first 64 sequences' counts stay in registers, so that up to there the search reads memory once.
+// and more.) The first 64 sequences' counts stay in registers, so that up to
+// there the search reads memory once.
 template <int kSrc, int kPer>
 __device__ __forceinline__ bool find_block(const RowsArgs& a, int item, SeqRows& sr, int& seq, int& qblk) {
   const int lane = threadIdx.x & 63;
@@ -220,7 +221,7 @@ __device__ __forceinline__ bool find_block(const RowsArgs& a, int item, SeqRows&
 // LDS of a workgroup: K and V tiles of 16-bit values, tile t in stage t %
 // kStages; for an 8-bit cache also the codes of a K and of a V tile on their way
 // (each wave's rows in turn; 80 KB with two stages, so that two workgroups fit a
-// CU), for packed rows a flag.
+// CU, 144 with four), for packed rows a flag.
 template <int kStages, bool kQ8>
 struct RowsLds {
   uint8_t k[kStages][kKT * kRowBytes];
@@ -238,7 +239,8 @@ struct RowsLds<kStages, true> {
 // which two share 32 rows, each with its half of every tile's keys, and are
 // merged at the end (few rows: a tile takes a wave half as long). With four
 // stages of K and V one workgroup fits a CU, with two stages and four waves two
-// do. A barrier every kBar tiles, half the stages.
+// do. A barrier every kBar tiles, half the stages (2033 rows over 8-bit pages:
+// 1454 us with two stages, 1392 with four).
 template <int kRows, int kSrc, bool kPaged>
 __global__ __launch_bounds__(kRows == 256 ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void k_rows_attn(RowsArgs a) {
@@ -247,7 +249,7 @@ void k_rows_attn(RowsArgs a) {
   constexpr bool kHalves = kRows == 64;
   // Keys of a tile that a wave takes, in 32s and 16s.
   constexpr int kMine32 = kHalves ? kKT32 / 2 : kKT32, kMine16 = 2 * kMine32;
-  constexpr int kStages = kRows == 256 && !kQ8 ? 4 : 2;
+  constexpr int kStages = kRows == 256 ? 4 : 2;
   // Weights and V: bf16, or over codes fp16.
   typedef std::conditional_t<kQ8, f16x8_t, bf16x8_t> P8;
   constexpr int kBar = kStages / 2;
@@ -399,8 +401,8 @@ void k_rows_attn(RowsArgs a) {
   // 8-bit cache. Lane i holds the page and the factors of block i of a window
   // of 64 blocks, which a wave takes with a lane read, with no load in the way;
   // the window moves by 32 blocks, the one after it on its way: the tile at hand
-  // lies in its first half, and the (at most 16) blocks of the next three
-  // tiles in it too. A block with a scale that is no finite number (it was made
+  // lies in its first half, and the blocks of the next four tiles (at most 20
+  // further on) in it too. A block with a scale that is no finite number (it was made
   // of rows that held one) is `odd`: it has NaN for its keys, so whoever sees
   // it gets NaN, and for the others its V counts as zero.
   const int mb0 = kQ8 ? k0 >> a.c.log2_block : 0, mlast = kQ8 ? (k1 - 1) >> a.c.log2_block : 0;
@@ -723,7 +725,7 @@ void k_rows_attn(RowsArgs a) {
     }
     l += ps;
     if (__builtin_expect(t0 + 2 * kKT > cut, 0)) mask(t0 + kKT, sn);
-    // The codes of K(ti + 2) and V(ti + 1), asked for a round ago.
+    // The codes of K(ti + kBar + 1) and V(ti + kBar), asked for a round ago.
     Codes wk, wv;
     if constexpr (kQ8) {
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
@@ -749,19 +751,19 @@ void k_rows_attn(RowsArgs a) {
           const int n = 4 * ks + dt;
 #pragma unroll
           for (int w = n * kWords / kMfmas; w < (n + 1) * kWords / kMfmas; ++w) {
-            if (w < 4 * kUnits) put_word(true, wk, w, st, four);
-            else put_word(false, wv, w - 4 * kUnits, (st + 1) % kStages, four);
+            if (w < 4 * kUnits) put_word(true, wk, w, (st + kBar + 1) % kStages, four);
+            else put_word(false, wv, w - 4 * kUnits, (st + kBar) % kStages, four);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     if constexpr (kQ8) {
-      put_odd(true, ti + 2, st);
-      put_odd(false, ti + 1, (st + 1) % kStages);
+      put_odd(true, ti + kBar + 1, (st + kBar + 1) % kStages);
+      put_odd(false, ti + kBar, (st + kBar) % kStages);
       compiler_fence();  // the codes have been read when the next are asked for
-      ask(true, ti + 3, raw_at(true));
-      ask(false, ti + 2, raw_at(false));
+      ask(true, ti + kBar + 2, raw_at(true));
+      ask(false, ti + kBar + 1, raw_at(false));
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -783,20 +785,30 @@ void k_rows_attn(RowsArgs a) {
   if constexpr (!kQ8) exchange_q();
   for (;;) {
     if constexpr (kQ8) {
-      // K(1) by way of the stage that V(1) has not been put into yet.
-      const uint32_t spare = __builtin_amdgcn_readfirstlane(lds0) + (uint32_t)offsetof(Lds, v[1]) + raw_of_wave;
+      // Beside K(0) and V(0), the first ones by way of the stages that nothing
+      // is put into yet.
+      const uint32_t spare_v = __builtin_amdgcn_readfirstlane(lds0) + (uint32_t)offsetof(Lds, v[kStages - 1]) + raw_of_wave;
+      const uint32_t spare_k = __builtin_amdgcn_readfirstlane(lds0) + (uint32_t)offsetof(Lds, k[kStages - 1]) + raw_of_wave;
       ask(true, 0, raw_at(true));
       ask(false, 0, raw_at(false));
-      ask(true, 1, spare);
+      ask(true, 1, spare_v);
+      if constexpr (kBar == 2) {
+        ask(true, 2, spare_v + kKT * kHeadDim);
+        ask(false, 1, spare_k);
+      }
       exchange_q();
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
       __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
       bare_barrier();  // codes go where queries were
       put(true, 0, raw_at(true), 0);
       put(false, 0, raw_at(false), 0);
-      put(true, 1, spare, 1);
-      ask(true, 2, raw_at(true));
-      ask(false, 1, raw_at(false));
+      put(true, 1, spare_v, 1);
+      if constexpr (kBar == 2) {
+        put(true, 2, spare_v + kKT * kHeadDim, 2);
+        put(false, 1, spare_k, 1);
+      }
+      ask(true, kBar + 1, raw_at(true));
+      ask(false, kBar, raw_at(false));
     } else {
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
     }
