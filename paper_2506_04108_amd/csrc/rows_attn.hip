@@ -44,7 +44,7 @@
 // cycles and the VALU 55 %).
 //
 // Measured: one prompt of 16384 tokens, 32 heads over 8: 1.86 ms, 1.18 PFLOP/s; 16
-// prompts of 77 to 2000 tokens, 28 heads over 4: 214 us, 0.78 PFLOP/s, of which a
+// prompts of 77 to 2000 tokens, 28 heads over 4: 212 us, 0.79 PFLOP/s, of which a
 // workgroup's start (its block, queries, first tiles) and end take 60; one of 300
 // tokens 10.2 us, a chain of latencies. 32 rows of 4 heads behind 8 x 64K codes:
 // 357 us with the stores and the merge, 3.0 TB/s; 2033 rows of 7 behind 31K:
@@ -75,6 +75,7 @@ constexpr int kKT32 = kKT / 32, kKT16 = kKT / 16;
 constexpr int kRowBytes = kHeadDim * 2;
 constexpr int kCus = 256;
 constexpr int kClassKeys = 1024;          // query blocks: a class of costs
+constexpr int kShortPrompt = 2560;         // tokens of a prompt on average, that are few
 constexpr int64_t kLongSplit = 1024;      // keys of a split that is long
 constexpr float kMaxWeightSum = 4096.f;
 constexpr int kPacked = -1;                // source of keys: packed bf16 rows, else the format of the 8-bit cache
@@ -154,9 +155,9 @@ __device__ __forceinline__ SeqRows seq_rows(const RowsArgs& a, int s) {
 // kClassKeys keys each, from the highest down, those of a class sequence by
 // sequence: workgroups that run together then share the keys of a sequence, in
 // the L2, and the last ones are short all the same. Against strictly falling
-// costs: 16 prompts of up to 2000 tokens, 28 heads over 4, 224 -> 214 us; 64 of up to
-// 700, 32 over 8, 233 -> 202; 30 of 1000, 8 over 8, whose last class is a larger part of
-// the whole, 63.5 -> 67.8. (Blocks of different costs next to each other: 16 prompts 259
+// costs, all by 256 rows: 16 prompts of up to 2000 tokens, 28 heads over 4, 224 -> 214
+// us; 64 of up to 700, 32 over 8, 233 -> 202; 30 of 1000, 8 over 8, whose last class is a
+// larger part of the whole, 63.5 -> 67.8. (Blocks of different costs next to each other: 16 prompts 259
 // and more.) The first 64 sequences' counts stay in registers, so that up to
 // there the search reads memory once.
 template <int kSrc, int kPer>
@@ -1059,8 +1060,13 @@ hipError_t launch_prompt(const RowsArgs& a, hipStream_t stream) {
   // a CU): 1000 tokens of 32 / 8 heads 27.3 us by 128 rows, 24.5 by 64; 8 prompts
   // of up to 250, whose 625 blocks do not, 15.3 and 19.6.
   if (most_blocks(a, 64) * a.kv_heads <= 2 * kCus) return launch_attn<64, kPacked, false>(a, stream);
-  return most_blocks(a, 256) * a.kv_heads < 2 * kCus ? launch_attn<128, kPacked, false>(a, stream)
-                                                     : launch_attn<256, kPacked, false>(a, stream);
+  // Two workgroups a CU while prompts are short (one computes while the other
+  // starts): 30 of 1000 tokens, 8 heads over 8, 67 us by 256 rows, 52 by 128; 64 of up
+  // to 700, 32 over 8, 200 and 191; 8 of up to 4000 446 and 437; 4 of 4000, 28 over 4, 452
+  // and 458; one of 16384 1912 and 1975.
+  return a.rows <= (int64_t)kShortPrompt * a.batch || most_blocks(a, 256) * a.kv_heads < 2 * kCus
+             ? launch_attn<128, kPacked, false>(a, stream)
+             : launch_attn<256, kPacked, false>(a, stream);
 }
 
 }  // namespace resa

@@ -190,3 +190,9 @@ def test_cache_whose_tensors_change():
     p.dev.block_table.set_(torch.full((1, 3), -1, dtype=torch.int32, device="cuda"))
     with pytest.raises((ValueError, R.ResaError)):
         R.load_rows_q8(p.dev, cu, lt, 50)
+
+
+@pytest.mark.parametrize("lens,hq,hkv,heads", [([6000, 1, 64, 0, 9001], 32, 8, [3, 30]), ([2561, 2600, 2599], 28, 4, [0, 27]),
+                                               ([8192], 8, 8, [7])])
+def test_prompts_long_on_average(lens, hq, hkv, heads):
+    run(lens, hq, hkv, seed=980, heads=heads)
