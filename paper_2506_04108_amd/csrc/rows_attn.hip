@@ -87,13 +87,6 @@ __host__ __device__ constexpr int swz(int r) { return ((r & 3) << 2) | ((r >> 2)
 
 // Rows of a workgroup (64, 128 or 256) and its waves.
 __host__ __device__ constexpr int waves_of(int rows) { return rows == 256 ? 8 : 4; }
-// Over a cache: as few as hold a sequence's rows. 32 rows of one head for each
-// of 8 kv heads behind 8 x 32K: 183 us by 128 rows, 146 by 64; 32 rows of four
-// behind 8 x 64K 381 and 505.
-int rows_of_block(int32_t batch, int32_t rows, int32_t group) {
-  const int64_t all = (int64_t)rows * group;
-  return all <= (int64_t)64 * batch ? 64 : all <= (int64_t)128 * batch ? 128 : 256;
-}
 
 constexpr int kWaitVm0 = kWaitVmcnt0;
 
@@ -1009,9 +1002,48 @@ hipError_t launch_attn(const RowsArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Workgroups of `per` rows over one split of the keys.
+int64_t rows_wgs(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int per) {
+  const int64_t each = ((int64_t)((rows + batch - 1) / batch) * group + per - 1) / per;
+  return (each < 1 ? 1 : each) * batch * kv_heads;
+}
+// Splits that fill `slots` places for workgroups once.
+int64_t splits_within(int64_t wgs, int64_t slots) { return wgs >= slots ? 1 : slots / wgs; }
+
+// Rows of a workgroup over a cache. Few rows a sequence: as few as hold them
+// (32 rows of one head for each of 8 kv heads behind 8 x 32K: 183 us by 128
+// rows, 146 by 64; 32 rows of four behind 8 x 64K 381 and 505). More: 256, which
+// share the conversion of the codes, where the rows fill three quarters of the
+// places (512 rows of 32 heads over 8 behind 32K: 288 us by 256, 320 by 128; 100
+// behind 8 x 8K 167 and 181), else 128, two workgroups a CU (54 rows of 40 behind
+// 6 x 3.5K 90 and 79; 340 of 16 over 4 behind 8 of up to 3.7K 127 and 114).
+int rows_of_block(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows) {
+  const int64_t all = (int64_t)rows * group;
+  if (all <= (int64_t)64 * batch) return 64;
+  if (all <= (int64_t)128 * batch) return 128;
+  const int64_t wgs = rows_wgs(batch, kv_heads, group, rows, 256), splits = splits_within(wgs, kCus);
+  const int64_t places = wgs * splits > kCus ? wgs * splits : kCus;
+  return 4 * all * kv_heads * splits >= 3 * 256 * places ? 256 : 128;
+}
+
+// Key splits at most. 256 rows: no more than run at once, one workgroup a CU
+// (93 rows of 12 heads over 2 behind 6 of up to 36K: 167 us with 7 splits, 252
+// workgroups; with 8, 288 workgroups, 273). Fewer: a workgroup on every CU at
+// least, and as many as run at once, two a CU, where a split stays long: every
+// split writes its rows' sums and the merge reads them again. 32 rows of 32 heads
+// behind 8K: 32.9 us with one workgroup a CU, 40.0 with two; behind 8 x 64K 444
+// and 384.
+int64_t rows_most_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
+  const int per = rows_of_block(batch, kv_heads, group, rows);
+  const int64_t wgs = rows_wgs(batch, kv_heads, group, rows, per);
+  if (per == 256) return splits_within(wgs, kCus);
+  const int64_t least = wgs >= kCus ? 1 : (kCus + wgs - 1) / wgs;
+  return max_seq_len >= kLongSplit * least ? splits_within(wgs, 2 * kCus) : least;
+}
+
 template <int kSrc, bool kPaged>
 hipError_t launch_q8(const RowsArgs& a, hipStream_t stream) {
-  const int rows = rows_of_block(a.batch, a.rows, a.group);
+  const int rows = rows_of_block(a.batch, a.kv_heads, a.group, a.rows);
   const hipError_t e = rows == 64    ? launch_attn<64, kSrc, kPaged>(a, stream)
                        : rows == 128 ? launch_attn<128, kSrc, kPaged>(a, stream)
                                      : launch_attn<256, kSrc, kPaged>(a, stream);
@@ -1022,18 +1054,6 @@ hipError_t launch_q8(const RowsArgs& a, hipStream_t stream) {
 }
 
 }  // namespace
-
-// Key splits at most: enough for a workgroup on every CU, and for a second one
-// (of 4 waves) where a split stays long: every split writes its rows' sums and
-// the merge reads them again. 32 rows of 32 heads behind 8K: 32.9 us with one
-// workgroup a CU, 40.0 with two; behind 8 x 64K 444 and 384.
-static int64_t rows_most_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
-  const int per = rows_of_block(batch, rows, group);
-  const int64_t each = ((int64_t)((rows + batch - 1) / batch) * group + per - 1) / per;
-  const int64_t wgs = (each < 1 ? 1 : each) * batch * kv_heads;
-  const auto splits = [&](int64_t want) { return wgs >= want ? 1 : (want + wgs - 1) / wgs; };
-  return per < 256 && max_seq_len >= kLongSplit * splits(kCus) ? splits(2 * kCus) : splits(kCus);
-}
 
 int32_t rows_chunk(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
   const int64_t most = rows_most_splits(batch, kv_heads, group, rows, max_seq_len);
