@@ -43,12 +43,13 @@
 // here too, as in long prompts (1.75 GHz, the matrix cores busy 64 % of the
 // cycles and the VALU 55 %).
 //
-// Measured: one prompt of 16384 tokens, 32 heads over 8: 1.86 ms, 1.18 PFLOP/s; 16
-// prompts of 77 to 2000 tokens, 28 heads over 4: 212 us, 0.79 PFLOP/s, of which a
-// workgroup's start (its block, queries, first tiles) and end take 60; one of 300
-// tokens 10.2 us, a chain of latencies. 32 rows of 4 heads behind 8 x 64K codes:
-// 357 us with the stores and the merge, 3.0 TB/s; 2033 rows of 7 behind 31K:
-// 1.39 ms, 0.99 PFLOP/s.
+// Measured: one prompt of 16384 tokens, 32 heads over 8: 1.85 - 1.88 ms, 1.17 - 1.19
+// PFLOP/s; 16 prompts of 77 to 2000 tokens, 28 heads over 4: 207 - 219 us, 0.76 -
+// 0.81 PFLOP/s, the starts and ends of workgroups (block, queries, first tiles;
+// output: 10 us each) not all hidden by their neighbours; one of 300 tokens 10.1 us, a
+// chain of latencies. 32 rows of 4 heads behind 8 x 64K codes: 357 - 374 us with
+// the stores and the merge, 2.9 - 3.0 TB/s; 2033 rows of 7 behind 31K: 1.39 - 1.41
+// ms, 0.98 - 1.0 PFLOP/s.
 //
 // Masked keys: scores are replaced, so nothing of a masked K row matters; a
 // masked V row meets weights of zero, which only a value that is not finite
