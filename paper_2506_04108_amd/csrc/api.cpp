@@ -772,20 +772,17 @@ bool rows_grid_fits(int32_t batch, int32_t rows, int32_t group, int32_t kv_heads
   return ((int64_t)rows * group / 128 + batch) * splits <= INT32_MAX / kv_heads;
 }
 
+// Workspace of an attention over packed rows: log-sum-exps of the splits, then
+// their outputs.
 struct RowsLayout {
-  int32_t chunk, splits;
-  size_t lse, o, total;
+  size_t o, total;
 };
 
-RowsLayout rows_layout(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
+RowsLayout rows_layout(int32_t q_heads, int32_t rows, int32_t splits) {
+  const size_t outs = (size_t)rows * q_heads;
   RowsLayout l;
-  l.chunk = resa::rows_chunk(batch, kv_heads, group, rows, max_seq_len);
-  l.splits = (max_seq_len + l.chunk - 1) / l.chunk;
-  if (l.splits < 1) l.splits = 1;
-  const size_t outs = (size_t)rows * kv_heads * group;
-  l.lse = 0;
-  l.o = round256(outs * l.splits * 4);
-  l.total = l.splits == 1 ? 0 : l.o + outs * l.splits * RESA_HEAD_DIM * 4;
+  l.o = round256(outs * splits * 4);
+  l.total = splits == 1 ? 0 : l.o + outs * splits * RESA_HEAD_DIM * 4;
   return l;
 }
 
@@ -903,10 +900,8 @@ size_t resa_rectify_q8_workspace_size(int32_t batch, int32_t num_kv_heads, int32
                                       int32_t max_seq_len) {
   if (batch < 1 || num_kv_heads < 1 || num_q_heads < num_kv_heads || num_rows < 1 || max_seq_len < 1) return 0;
   const int32_t group = num_q_heads / num_kv_heads;
-  const size_t most = (size_t)resa::rows_max_splits(batch, num_kv_heads, group, num_rows, max_seq_len);
-  if (most == 1) return 0;
-  const size_t outs = (size_t)num_rows * num_kv_heads * group;
-  return round256(outs * most * 4) + outs * most * RESA_HEAD_DIM * 4;
+  const int32_t most = resa::rows_max_splits(batch, num_kv_heads, group, num_rows, max_seq_len);
+  return rows_layout(num_kv_heads * group, num_rows, most).total;
 }
 
 int resa_dense_rectify_q8(const resa_kv_cache_q8_t* c, const void* q_rows, const void* k_rows, const void* v_rows,
@@ -927,16 +922,23 @@ int resa_dense_rectify_q8(const resa_kv_cache_q8_t* c, const void* q_rows, const
     return fail(RESA_ERR_INVALID_ARG, "max_seq_len %d outside [1, capacity %d]", max_seq_len, b->capacity);
   if (!std::isfinite(sm_scale)) return fail(RESA_ERR_INVALID_ARG, "sm_scale is not finite");
   if (num_rows == 0) return ok();
-  const RowsLayout lay = rows_layout(b->batch, b->num_kv_heads, group, num_rows, max_seq_len);
-  if (num_rows > INT32_MAX / RESA_MAX_GROUP || !rows_grid_fits(b->batch, num_rows, group, b->num_kv_heads, lay.splits))
+  resa::RowsArgs a = {};
+  a.batch = b->batch;
+  a.rows = num_rows;
+  a.q_heads = num_q_heads;
+  a.kv_heads = b->num_kv_heads;
+  a.group = group;
+  resa::rows_splits(&a, max_seq_len);
+  if (num_rows > INT32_MAX / RESA_MAX_GROUP ||
+      !rows_grid_fits(b->batch, num_rows, group, b->num_kv_heads, a.num_splits))
     return fail(RESA_ERR_UNSUPPORTED, "%d rows of %d heads are more than one launch takes", num_rows, num_q_heads);
+  const RowsLayout lay = rows_layout(num_q_heads, num_rows, a.num_splits);
   if (lay.total > 0 && (workspace == nullptr || workspace_bytes < lay.total))
     return fail(RESA_ERR_WORKSPACE, "rectify workspace needs %zu bytes, got %zu", lay.total,
                 workspace == nullptr ? (size_t)0 : workspace_bytes);
   if (workspace != nullptr && !aligned(workspace, 16))
     return fail(RESA_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
   char* ws = static_cast<char*>(workspace);
-  resa::RowsArgs a = {};
   a.c = store.c;
   a.k_scale = c->k_scale;
   a.v_scale = c->v_scale;
@@ -944,18 +946,11 @@ int resa_dense_rectify_q8(const resa_kv_cache_q8_t* c, const void* q_rows, const
   a.q = static_cast<const uint16_t*>(q_rows);
   a.q_stride = q_stride;
   a.cu = cu_rows;
-  a.batch = b->batch;
-  a.rows = num_rows;
-  a.q_heads = num_q_heads;
-  a.kv_heads = b->num_kv_heads;
-  a.group = group;
-  a.chunk = lay.chunk;
-  a.num_splits = lay.splits;
   a.scale_log2 = sm_scale * 1.4426950408889634f;
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
-  if (lay.splits > 1) {
-    a.part_lse = reinterpret_cast<float*>(ws + lay.lse);
+  if (a.num_splits > 1) {
+    a.part_lse = reinterpret_cast<float*>(ws);
     a.part_o = reinterpret_cast<float*>(ws + lay.o);
   }
   hipError_t e = resa::launch_store_rows_q8(store, static_cast<hipStream_t>(stream));

@@ -176,7 +176,8 @@ struct RowsArgs {
   int64_t q_stride, k_stride, v_stride;
   const int32_t* cu;           // [batch + 1]
   int32_t batch, rows, q_heads, kv_heads, group;
-  int32_t chunk, num_splits;   // keys per split, splits
+  int32_t chunk, num_splits;   // keys per split of equal lengths, splits at most
+  int32_t per, places, even_splits;  // 8-bit cache: rows and places of workgroups, splits of equal lengths
   float scale_log2;
   uint16_t* out;               // [rows, Hq, D]
   float* lse;                  // [rows, Hq] or null
@@ -208,7 +209,7 @@ int32_t select_blocks_per_wg(int32_t batch, int32_t kv_heads, int32_t max_blocks
 int32_t select_hist_words(int32_t batch, int32_t kv_heads, int32_t max_blocks_seq);
 int32_t decode_auto_splits(int32_t batch, int32_t kv_heads, int32_t n_cap, int32_t block_size);
 int32_t decode_q8_auto_splits(int32_t batch, int32_t kv_heads, int32_t n_cap, int32_t block_size);
-int32_t rows_chunk(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len);
+void rows_splits(RowsArgs* a, int32_t max_seq_len);
 int32_t rows_max_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len);
 int32_t rectify_num_qblocks(int32_t group, int32_t f);
 int32_t rectify_chunk(int32_t batch, int32_t kv_heads, int32_t rows, int32_t max_seq_len, bool masked);

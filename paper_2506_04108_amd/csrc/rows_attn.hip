@@ -56,6 +56,7 @@
 // would survive. The tiles that some row of the workgroup masks are searched
 // for such values, and a workgroup that finds one takes its range again, a
 // tile at a time, with these values apart.
+#include <algorithm>
 #include <type_traits>
 
 #include "rows_device.h"
@@ -213,6 +214,65 @@ __device__ __forceinline__ bool find_block(const RowsArgs& a, int item, SeqRows&
   return true;
 }
 
+// Keys of a split. Of one length every sequence would take a.chunk; where the
+// lengths differ, the longer ones are cut further, as long as all workgroups run
+// at once (a.places), into at most a.num_splits: sum of blocks (tiles / t + 1) <=
+// places for t = tiles / (places - blocks). 6 sequences of up to 36K, 93 rows of 12
+// heads over 2: 165 -> 130 us; 8 of 8K, 100 rows of 32 over 8, for which nothing
+// changes but the search, 172 -> 177. `q0` and `nb0` are this lane's sequence
+// and its blocks.
+template <int kSrc>
+__device__ __forceinline__ int split_chunk(const RowsArgs& a, const SeqRows& q0, int nb0) {
+  if (a.batch == 1) return a.chunk;
+  const int lane = threadIdx.x & 63, shift = __builtin_ctz(a.per);
+  int tiles = nb0 * ((q0.L + kKT - 1) / kKT), blocks = nb0, longest = nb0 == 0 ? 0 : q0.L;
+  if (nb0 == 0) tiles = 0;
+  for (int base = 64; base < a.batch; base += 64) {
+    if (base + lane >= a.batch) continue;
+    const SeqRows q = seq_rows<kSrc>(a, base + lane);
+    const int nb = (q.n * a.group + a.per - 1) >> shift;
+    if (nb == 0) continue;
+    tiles += nb * ((q.L + kKT - 1) / kKT);
+    blocks += nb;
+    longest = max(longest, q.L);
+  }
+  const int free = a.places / a.kv_heads - wave_total(blocks);
+  if (free <= 0) return a.chunk;
+  const int most = (int)wave_max((uint32_t)longest), sum = wave_total(tiles);
+  const int t = max(max((sum + free - 1) / free, (most + kKT * a.num_splits - 1) / (kKT * a.num_splits)), 2);
+  return min(a.chunk, t * kKT);
+}
+template <int kSrc>
+__device__ __forceinline__ int splits_of(const RowsArgs& a, int L, int chunk) {
+  return min((L + chunk - 1) / chunk, a.num_splits);
+}
+
+// Query block and split `item`, sequence by sequence (all splits are about as
+// long).
+template <int kSrc, int kPer>
+__device__ __forceinline__ bool find_split(const RowsArgs& a, int item, SeqRows& sr, int& seq, int& qblk, int& split,
+                                           int& chunk) {
+  const int lane = threadIdx.x & 63;
+  auto rows_at = [&](int s) -> SeqRows { return s < a.batch ? seq_rows<kSrc>(a, s) : SeqRows{0, 0, 0}; };
+  auto blocks = [&](const SeqRows& q) -> int { return (q.n * a.group + kPer - 1) / kPer; };
+  const SeqRows q0 = rows_at(lane);
+  chunk = split_chunk<kSrc>(a, q0, blocks(q0));
+  auto count = [&](int s) -> int {
+    const SeqRows q = s < 64 ? q0 : rows_at(s);
+    const int nb = blocks(q);
+    return nb == 0 ? 0 : nb * splits_of<kSrc>(a, q.L, chunk);
+  };
+  int rank;
+  if (!find_seq(item, a.batch, count, seq, rank)) return false;
+  sr = seq < 64 ? SeqRows{__builtin_amdgcn_readlane(q0.first, seq & 63), __builtin_amdgcn_readlane(q0.n, seq & 63),
+                          __builtin_amdgcn_readlane(q0.L, seq & 63)}
+                : seq_rows<kSrc>(a, seq);
+  const int S = splits_of<kSrc>(a, sr.L, chunk);
+  qblk = rank / S;
+  split = rank - qblk * S;
+  return true;
+}
+
 // LDS of a workgroup: K and V tiles of 16-bit values, tile t in stage t %
 // kStages; for an 8-bit cache also the codes of a K and of a V tile on their way
 // (each wave's rows in turn; 80 KB with two stages, so that two workgroups fit a
@@ -256,17 +316,21 @@ void k_rows_attn(RowsArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rwave = kHalves ? wave & 1 : wave, half = kHalves ? wave >> 1 : 0;
   const int S = a.num_splits, G = a.group;
-  const int hk = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % S;
-  int seq, qblk;
+  const int hk = blockIdx.x % a.kv_heads, item = blockIdx.x / a.kv_heads;
+  int seq, qblk, split = 0, chunk = a.chunk;
   SeqRows sr;
-  if (!find_block<kSrc, kRows>(a, rest / S, sr, seq, qblk)) return;
+  if (kQ8 && S > 1) {
+    if (!find_split<kSrc, kRows>(a, item, sr, seq, qblk, split, chunk)) return;
+  } else if (!find_block<kSrc, kRows>(a, item, sr, seq, qblk)) {
+    return;
+  }
   if constexpr (!kQ8) {
     if (tid == 0) lds.odd = 0;
   }
   const int R = sr.n * G, past = sr.L - sr.n;
-  const int k0 = split * a.chunk;
+  const int k0 = split * chunk;
   const int last_row = min(R - 1, (qblk + 1) * kRows - 1);
-  const int k1 = min(min(k0 + a.chunk, sr.L), past + last_row / G + 1);
+  const int k1 = min(min(k0 + chunk, sr.L), past + last_row / G + 1);
   if (k1 <= k0) return;  // no key of this split is seen: the merge does not read it
   const int ntiles = (k1 - k0 + kKT - 1) / kKT;
   const float ninf = -__builtin_inff();
@@ -948,10 +1012,11 @@ __global__ __launch_bounds__(256) void k_rows_combine(RowsArgs a) {
   if (row >= a.rows) return;
   // The sequence whose packed rows hold this row.
   int seq = -1;
+  const SeqRows q0 = lane < a.batch ? seq_rows<kSrc>(a, lane) : SeqRows{0, 0, 0};
   for (int base = 0; base < a.batch && seq < 0; base += 64) {
     bool mine = false;
     if (base + lane < a.batch) {
-      const SeqRows q = seq_rows<kSrc>(a, base + lane);
+      const SeqRows q = base == 0 ? q0 : seq_rows<kSrc>(a, base + lane);
       mine = row >= q.first && row < q.first + q.n;
     }
     const uint64_t who = __ballot(mine);
@@ -960,7 +1025,8 @@ __global__ __launch_bounds__(256) void k_rows_combine(RowsArgs a) {
   if (seq < 0) return;
   const SeqRows sr = seq_rows<kSrc>(a, seq);
   const int keys = sr.L - sr.n + (row - sr.first) + 1;
-  const int n = min((keys + a.chunk - 1) / a.chunk, a.num_splits);
+  const int chunk = split_chunk<kSrc>(a, q0, (q0.n * a.group + a.per - 1) >> __builtin_ctz(a.per));
+  const int n = splits_of<kSrc>(a, keys, chunk);
   const size_t stride = (size_t)a.rows * a.q_heads;
   const float ninf = -__builtin_inff();
   float m = ninf, l = 0.f;
@@ -997,7 +1063,10 @@ int64_t most_blocks(const RowsArgs& a, int per) { return (int64_t)a.rows * a.gro
 
 template <int kRows, int kSrc, bool kPaged>
 hipError_t launch_attn(const RowsArgs& a, hipStream_t stream) {
-  const int64_t grid = most_blocks(a, kRows) * a.num_splits * a.kv_heads;
+  // Of one length, every block takes as many splits of a.chunk as the longest.
+  int64_t items = most_blocks(a, kRows);
+  if (a.num_splits > 1) items = std::max<int64_t>(items * a.even_splits, a.places / a.kv_heads);
+  const int64_t grid = items * a.kv_heads;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   hipLaunchKernelGGL((k_rows_attn<kRows, kSrc, kPaged>), dim3((uint32_t)grid), dim3(64 * waves_of(kRows)), 0, stream, a);
   return hipGetLastError();
@@ -1034,20 +1103,24 @@ int rows_of_block(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows) 
 // split writes its rows' sums and the merge reads them again. 32 rows of 32 heads
 // behind 8K: 32.9 us with one workgroup a CU, 40.0 with two; behind 8 x 64K 444
 // and 384.
-int64_t rows_most_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
+struct RowsPlan {
+  int per;
+  int64_t splits, places;
+};
+RowsPlan rows_plan(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
   const int per = rows_of_block(batch, kv_heads, group, rows);
   const int64_t wgs = rows_wgs(batch, kv_heads, group, rows, per);
-  if (per == 256) return splits_within(wgs, kCus);
+  if (per == 256) return {per, splits_within(wgs, kCus), kCus};
   const int64_t least = wgs >= kCus ? 1 : (kCus + wgs - 1) / wgs;
-  return max_seq_len >= kLongSplit * least ? splits_within(wgs, 2 * kCus) : least;
+  const bool is_long = max_seq_len >= kLongSplit * least;
+  return {per, is_long ? splits_within(wgs, 2 * kCus) : least, is_long ? 2 * kCus : wgs * least};
 }
 
 template <int kSrc, bool kPaged>
 hipError_t launch_q8(const RowsArgs& a, hipStream_t stream) {
-  const int rows = rows_of_block(a.batch, a.kv_heads, a.group, a.rows);
-  const hipError_t e = rows == 64    ? launch_attn<64, kSrc, kPaged>(a, stream)
-                       : rows == 128 ? launch_attn<128, kSrc, kPaged>(a, stream)
-                                     : launch_attn<256, kSrc, kPaged>(a, stream);
+  const hipError_t e = a.per == 64    ? launch_attn<64, kSrc, kPaged>(a, stream)
+                       : a.per == 128 ? launch_attn<128, kSrc, kPaged>(a, stream)
+                                      : launch_attn<256, kSrc, kPaged>(a, stream);
   if (e != hipSuccess || a.num_splits == 1) return e;
   const int64_t outs = (int64_t)a.rows * a.q_heads;
   hipLaunchKernelGGL(k_rows_combine<kSrc>, dim3((uint32_t)((outs + 3) / 4)), dim3(256), 0, stream, a);
@@ -1056,18 +1129,24 @@ hipError_t launch_q8(const RowsArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-int32_t rows_chunk(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
-  const int64_t most = rows_most_splits(batch, kv_heads, group, rows, max_seq_len);
-  int64_t chunk = ((max_seq_len + most - 1) / most + 63) / 64 * 64;
-  return (int32_t)(chunk < 128 ? 128 : chunk);
+void rows_splits(RowsArgs* a, int32_t max_seq_len) {
+  const RowsPlan p = rows_plan(a->batch, a->kv_heads, a->group, a->rows, max_seq_len);
+  const int64_t chunk = ((max_seq_len + p.splits - 1) / p.splits + 63) / 64 * 64;
+  a->chunk = (int32_t)(chunk < 128 ? 128 : chunk);
+  a->per = p.per;
+  a->places = (int32_t)p.places;
+  a->even_splits = (int32_t)(((int64_t)max_seq_len + a->chunk - 1) / a->chunk);
+  a->num_splits = a->even_splits == 1 ? 1 : rows_max_splits(a->batch, a->kv_heads, a->group, a->rows, max_seq_len);
 }
 
-// A bound on the splits that never decreases as the length grows.
+// A bound on the splits that never decreases as the length grows: twice those
+// of equal lengths, of 128 keys at least.
 int32_t rows_max_splits(int32_t batch, int32_t kv_heads, int32_t group, int32_t rows, int32_t max_seq_len) {
-  const int64_t most = rows_most_splits(batch, kv_heads, group, rows, max_seq_len);
+  const int64_t most = rows_plan(batch, kv_heads, group, rows, max_seq_len).splits;
   const int64_t by_len = ((int64_t)max_seq_len + 127) / 128;
-  const int64_t s = by_len < most ? by_len : most;
-  return (int32_t)(s < 1 ? 1 : s);
+  if (most == 1 || by_len <= 1) return 1;
+  const int64_t s = batch == 1 ? most : 2 * most;
+  return (int32_t)(by_len < s ? by_len : s);
 }
 
 hipError_t launch_rows_q8(const RowsArgs& a, int32_t format, hipStream_t stream) {

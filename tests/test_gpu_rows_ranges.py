@@ -196,3 +196,18 @@ def test_cache_whose_tensors_change():
                                                ([8192], 8, 8, [7])])
 def test_prompts_long_on_average(lens, hq, hkv, heads):
     run(lens, hq, hkv, seed=980, heads=heads)
+
+
+@pytest.mark.parametrize("lens,n,g", [([12000, 100, 3000, 17, 700, 5], [20, 20, 0, 17, 9, 5], 4),
+                                      ([200, 15000, 64, 1], [90, 60, 64, 1], 8),
+                                      ([9000, 300], [700, 300], 3), ([33] * 80 + [7000, 2], [3] * 80 + [16, 2], 4)])
+@pytest.mark.parametrize("paged", [False, True])
+def test_rectify_lengths_far_apart(lens, n, g, paged):
+    """The long sequences take more splits than the short ones."""
+    H = 1 if len(lens) > 10 else 2
+    p = filled(len(lens), H, 32, "int8" if paged else "e4m3", lens, 990, paged)
+    ws = R.Workspace("cuda")
+    for _ in range(2):
+        q, cu, out, lse = rectify(p, lens, n, H * g, 991, ws=ws)
+        rectify_check(p, q, cu, lens, out, lse, f"lens={lens[:6]} n={n[:6]} g={g} paged={paged}", heads=[0, H * g - 1])
+    p.same(lens, "lengths far apart")
