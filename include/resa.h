@@ -420,7 +420,7 @@ typedef struct resa_kv_cache_q8 {
   resa_kv_cache_t base;
   float* k_scale;       /* fp32 [batch, num_kv_heads, capacity / block_size]; paged:
                            [num_pages, num_kv_heads] */
-  float* v_scale;       /* same layout */
+  float* v_scale;       /* same layout; scales are not negative */
   int32_t format;       /* resa_q8_format_t */
 } resa_kv_cache_q8_t;
 
@@ -494,9 +494,13 @@ size_t resa_rectify_q8_workspace_size(int32_t batch, int32_t num_kv_heads, int32
  * max_seq_len (host) bounds every seq_lens[s] and lies in [1, capacity]. Rows
  * of sequences that the store leaves as they are, and of none, keep their out
  * and lse. A block whose scale is not finite makes the rows that see one of
- * its keys NaN, and no others. Precision as in resa_prompt_attention. The
- * workspace holds split partials and needs no initialisation; calls sharing it
- * must be ordered on one stream.
+ * its keys NaN, and no others. Precision: scores, softmax and sums in fp32, the
+ * weights rounded to fp16 for the second product, out rounded to bf16. A weight
+ * is off by 2^-11 of itself or, where that is less, 2^-18 of the row's largest
+ * (value scales within 2^6 of each other) or 2^-39 of the largest of its 16 keys
+ * (further apart); values up to 2^-100 may count as zero beside larger ones.
+ * Finite for |v| <= 2^96. The workspace holds split partials and needs no
+ * initialisation; calls sharing it must be ordered on one stream.
  */
 int resa_dense_rectify_q8(const resa_kv_cache_q8_t* c, const void* q_rows, const void* k_rows,
                           const void* v_rows, int64_t q_stride, int64_t k_stride, int64_t v_stride,

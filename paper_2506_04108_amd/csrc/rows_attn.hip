@@ -34,8 +34,11 @@
 //
 // 8-bit cache: every code is a bf16 and an fp16 value, so both products are on
 // the codes themselves; a block's key scale multiplies the score (inside the fma
-// of the weight) and its value scale the weight, which is fp16 here (2^-11: the
-// result's own rounding is the larger by far). The codes go from HBM into LDS,
+// of the weight) and its value scale, over a power of two that all keys share, the
+// weight, which is fp16 here (2^-11: the result's own rounding is the larger by
+// far). Where the value scales of a split lie more than 2^6 apart, the product of
+// each 16 keys is taken by itself, so that a row of small values keeps its bits:
+// 8 x 64K 363 -> 548 us, 2033 rows behind 31K 1410 -> 2655. The codes go from HBM into LDS,
 // a round later through registers, converted under P.V's MFMAs, into the tiles.
 // 8 x 64K, 32 rows of 4 heads each: 402 -> 370 us a call against codes and
 // scales held in registers on their way (whose copies from one register to
@@ -80,6 +83,7 @@ constexpr int kClassKeys = 1024;          // query blocks: a class of costs
 constexpr int kShortPrompt = 2560;         // tokens of a prompt on average, that are few
 constexpr int64_t kLongSplit = 1024;      // keys of a split that is long
 constexpr float kMaxWeightSum = 4096.f;
+constexpr int kUnitRange = 7;             // value scales (log2) that share a unit
 constexpr int kPacked = -1;                // source of keys: packed bf16 rows, else the format of the 8-bit cache
 
 // Rows of a tile are 256 B; 16-byte piece p of row r sits in slot p ^ swz(r),
@@ -306,6 +310,7 @@ void k_rows_attn(RowsArgs a) {
   constexpr int kMine32 = kHalves ? kKT32 / 2 : kKT32, kMine16 = 2 * kMine32;
   constexpr int kStages = kRows == 256 ? 4 : 2;
   // Weights and V: bf16, or over codes fp16.
+  typedef std::conditional_t<kQ8, _Float16, __bf16> Weight;
   typedef std::conditional_t<kQ8, f16x8_t, bf16x8_t> P8;
   constexpr int kBar = kStages / 2;
   constexpr int kLoadRows = kKT / kWaves;  // tile rows whose K and V each wave brings in
@@ -626,27 +631,56 @@ void k_rows_attn(RowsArgs a) {
     return f;
   };
   // fp16 weights carry the value scale over vref, a power of two above the
-  // largest value scale met so far, which the accumulators are in units of.
-  uint32_t vref = 0x00800000u;  // bits of 2^-126
+  // largest one of the split, which the accumulators are in units of. A row may
+  // see none of that block, or give it no weight. So this is done only where all
+  // scales lie within 2^kUnitRange of vref: a weight then is off by 2^-25
+  // 2^kUnitRange at most, where the row's largest is 1 or more. Elsewhere (`apart`)
+  // vref is 1 and the product of each block is taken by itself.
+  uint32_t vref = 0x3f800000u;  // bits of it
+  bool apart = false;
+  // The bounds of the split's value scales, found by the waves together: each
+  // looks at every kWaves-th 64 blocks and leaves what it finds in LDS that no
+  // tile is put into before the second barrier. Blocks of values up to 2^-100
+  // (zeros as a rule) and odd ones set no lower bound.
+  constexpr uint32_t kNoScale = __builtin_bit_cast(uint32_t, kQ8Least / Q8<kQ8 ? kSrc : 0>::kMax) + 1;
+  auto bounds_at = [&]() __attribute__((always_inline)) -> uint32_t* {
+    return reinterpret_cast<uint32_t*>((kBar == 1 ? lds.v[kStages - 1] : lds.k[kStages - 1]) + kKT * kHeadDim);
+  };
+  auto look_at_scales = [&]() __attribute__((always_inline)) {
+    if constexpr (kQ8) {
+      uint32_t top = 0, low = 0;  // low: of the inverted bits
+      auto look = [&](const Window& w) __attribute__((always_inline)) {
+        const uint32_t x = __float_as_uint(w.vf);  // in the order of bit patterns: scales are not negative
+        if (finite_f(w.vf) && finite_f(w.kf)) {
+          top = max(top, x);
+          low = max(low, x > kNoScale ? ~x : 0u);
+        }
+      };
+#pragma unroll 4
+      for (int base = 64 * wave; base <= mlast - mb0; base += 64 * kWaves) look(load_window(base));
+      top = wave_max(top);
+      low = wave_max(low);
+      if (lane == 0) {
+        bounds_at()[2 * wave] = top;
+        bounds_at()[2 * wave + 1] = low;
+      }
+    }
+  };
+  auto take_bounds = [&]() __attribute__((always_inline)) {
+    if constexpr (kQ8) {
+      const uint2 mine = *reinterpret_cast<const uint2*>(bounds_at() + 2 * (lane & (kWaves - 1)));
+      const uint32_t top = wave_max(mine.x), low = wave_max(mine.y);
+      const uint32_t up = (top & 0x7f800000u) + 0x00800000u;
+      apart = low != 0 && (~low >> 23) + kUnitRange < up >> 23;
+      if (!apart) vref = up;
+    }
+  };
   auto value_factors = [&](int ti) __attribute__((always_inline)) -> Factors {
     Factors f;
     if constexpr (kQ8) {
-      uint32_t x[kKT16], top = 0;
-#pragma unroll
-      for (int i = 0; i < kKT16; ++i) {
-        x[i] = __float_as_uint(lane_f(win.vf, block_at(ti * kKT + 16 * i)));
-        top = max(top, x[i]);  // of bit patterns: scales are not negative
-      }
-      if (__builtin_expect(top > vref, 0)) {
-        const uint32_t up = (top & 0x7f800000u) + 0x00800000u;
-        const float alpha = __uint_as_float(vref) / __uint_as_float(up);
-        vref = up;
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
-      }
       const float inv = __uint_as_float(0x7f000000u - vref);  // 1 / vref
 #pragma unroll
-      for (int i = 0; i < kMine16; ++i) f.x[i] = __uint_as_float(half != 0 ? x[i + kKT16 - kMine16] : x[i]) * inv;
+      for (int i = 0; i < kMine16; ++i) f.x[i] = lane_f(win.vf, block_at(ti * kKT + 32 * half + 16 * i)) * inv;
     }
     return f;
   };
@@ -707,6 +741,81 @@ void k_rows_attn(RowsArgs a) {
     }
     __builtin_amdgcn_s_setprio(0);
     return (ps[0] + ps[1]) + (ps[2] + ps[3]);
+  };
+  // P.V of one tile whose value scales (g) have any sizes: for each 16 keys, which
+  // have one scale, the row's weights in units of a power of two that brings the
+  // largest to 2^14 .. 2^15 (fp16 ends at 2^16), a product of their own, and that
+  // added in fp32 times unit and scale. What a row adds up so is off by 2^-11 of
+  // itself, whatever other rows see. Gives the sum of the weights.
+  auto products_apart = [&](int st, const f32x16_t (&s)[kMine32], const Factors& f, const Factors& g)
+                            __attribute__((always_inline)) -> float {
+    constexpr uint32_t kLeastUnit = 15u << 23;  // 2^-112: its inverse is finite
+    const float mref = m == ninf ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < kMine16; ++ks) {
+      float p[8], pm = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int at = 8 * ks + i;
+        p[i] = fast_exp2(sub_rounded(s[at >> 4][at & 15] * f.x[ks], mref));
+        pm = fmaxf(pm, p[i]);
+        sum += p[i];
+      }
+      const uint32_t e = max(__float_as_uint(max_xor32(pm)) & 0x7f800000u, kLeastUnit);
+      const float up = __uint_as_float((268u << 23) - e);  // 2^14 over the unit e
+      const float back = __uint_as_float(e - (14u << 23)) * g.x[ks];
+      P8 w;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = (Weight)(p[i] * up);
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        f32x16_t part;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) part[i] = 0.f;
+        part = mfma32(read_v32(st, ks, dt), w, part);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = fmaf(part[i], back, o[dt][i]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    return sum;
+  };
+  // The split's tiles one after the other, for value scales of any sizes: the
+  // codes of the next tile on their way while one is worked on, K and V tiles in
+  // two stages, so that one barrier a tile is enough.
+  auto walk_apart = [&]() __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int ti = 0; ti < ntiles; ++ti) {
+      const int st = ti & 1, t0 = k0 + ti * kKT;
+      if (block_at(ti * kKT) >= 32) {
+        wbase += 32;
+        take_window(coming);
+        coming = load_window(wbase + 32);
+      }
+      __builtin_amdgcn_s_waitcnt(kWaitVm0);
+      put(true, ti, raw_at(true), st);
+      put(false, ti, raw_at(false), st);
+      ask(true, ti + 1, raw_at(true));
+      ask(false, ti + 1, raw_at(false));
+      __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+      bare_barrier();
+      f32x16_t s[kMine32];
+      fresh(kbase);
+      fresh(vbase);
+      scores(st, s);
+      if (t0 + kKT > cut) mask(t0, s);
+      const Factors f = key_factors(ti), g = value_factors(ti);
+      const float mn = fmaxf(m, row_max(s, f));
+      const float alpha = m == mn ? 1.f : fast_exp2(m - mn);
+      m = mn;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
+      l = l * alpha + products_apart(st, s, f, g);
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    bare_barrier();
   };
   // One tile: its weights (scores s) with the next tile's scores (sn), then
   // its P.V.
@@ -856,9 +965,15 @@ void k_rows_attn(RowsArgs a) {
         ask(false, 1, spare_k);
       }
       exchange_q();
+      look_at_scales();
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
       __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
       bare_barrier();  // codes go where queries were
+      take_bounds();
+      if (__builtin_expect(apart, 0)) {
+        walk_apart();
+        break;
+      }
       put(true, 0, raw_at(true), 0);
       put(false, 0, raw_at(false), 0);
       put(true, 1, spare_v, 1);
