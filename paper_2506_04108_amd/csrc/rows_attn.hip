@@ -497,7 +497,8 @@ void k_rows_attn(RowsArgs a) {
     const bool bad = !finite_f(w.kf) || !finite_f(w.vf);
     odd = __ballot(bad);
     win.page = w.page;
-    win.kf = bad ? c : w.kf * c;
+    // Never zero, so that a masked score stays -inf under it.
+    win.kf = bad ? c : fmaxf(w.kf * c, 0x1p-126f);
     win.vf = bad ? 0.f : w.vf;
   };
   // Block of key k0 + key (key a multiple of 16) in the window.
