@@ -491,6 +491,12 @@ void k_rows_attn(RowsArgs a) {
     }
     w.kf = a.k_scale[si];
     w.vf = a.v_scale[si];
+    // A page outside the pool reads as zeros, whatever the page looked at
+    // instead belongs to.
+    if (kPaged && w.page < 0) {
+      w.kf = 1.f;
+      w.vf = 0.f;
+    }
     return w;
   };
   auto take_window = [&](const Window& w) __attribute__((always_inline)) {
