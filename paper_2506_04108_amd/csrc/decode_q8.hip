@@ -31,7 +31,8 @@
 // terms of the 8 heads and columns 8 .. 15 the second; products are exact and
 // sums fp32, so results have fp32's precision. The unit 2^-k of w belongs to a
 // head: one that sees small values alone keeps their precision whatever the
-// others see. It and the softmax reference move rarely (only then are the
+// others see, and follows the reference: a value that had all the weight until a
+// far higher score came does not hold it. Both move rarely (only then are the
 // accumulators touched).
 //
 // Bound by HBM (256 B a token and kv head) and, with few chunks a wave, by the
@@ -227,7 +228,7 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
   // the sum of the weights.
   float m = ninf, l = 0.f;
   int k = 0;
-  bool none = true;  // no weight met yet: k says nothing
+  float most = 0.f;  // the w that k was last made for, under today's reference
   f32x4_t o[8];      // in units of 2^-k
 #pragma unroll
   for (int d = 0; d < 8; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -273,9 +274,11 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
     const float cm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     // The reference moves only when a score exceeds it by more than
     // kRefSlack, so the reduction over the column and the rescale are rare.
-    if (__any(cm > m + kRefSlack)) {
+    const bool moves = __any(cm > m + kRefSlack);
+    if (moves) {
       const float alpha = move_ref(m, max_xor32(max_xor16(cm)));
       l *= alpha;
+      most *= alpha;
 #pragma unroll
       for (int d = 0; d < 8; ++d) o[d] *= alpha;
     }
@@ -290,14 +293,14 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
       w[j] = p[j] * f[j >> 2];
       wm = fmaxf(wm, w[j]);
     }
-    if (__any(none || wm >= (float)(1 << kMost))) {
+    // The unit is made anew where a w outgrows it, and where the reference has
+    // moved: what the head summed up so far has shrunk beside the weights to come.
+    if (moves || __any(!(most > 0.f) || wm >= (float)(1 << kMost))) {
       float y = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) y = fmaxf(y, p[j] * vs[j >> 2]);
-      y = max_xor32(max_xor16(y));
-      const int want = kTop + 127 - (int)((__float_as_uint(y) >> 23) & 0xffu);
-      const int to = !(y > 0.f) ? k : none ? want : min(k, want);
-      none = none && !(y > 0.f);
+      most = fmaxf(most, max_xor32(max_xor16(y)));
+      const int to = most > 0.f ? kTop + 127 - (int)((__float_as_uint(most) >> 23) & 0xffu) : k;
 #pragma unroll
       for (int d = 0; d < 8; ++d)
 #pragma unroll
