@@ -287,7 +287,8 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
 #pragma unroll
     for (int j = 0; j < 8; ++j) p[j] = fast_exp2(x[j] - mref);
     l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-    float f[2] = {__builtin_ldexpf(vs[0], k), __builtin_ldexpf(vs[1], k)}, wm = 0.f;
+    const float f[2] = {__builtin_ldexpf(vs[0], k), __builtin_ldexpf(vs[1], k)};
+    float wm = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       w[j] = p[j] * f[j >> 2];
@@ -295,7 +296,8 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
     }
     // The unit is made anew where a w outgrows it, and where the reference has
     // moved: what the head summed up so far has shrunk beside the weights to come.
-    if (moves || __any(!(most > 0.f) || wm >= (float)(1 << kMost))) {
+    // A scale that is past fp32 in it comes here too.
+    if (moves || __any(!(most > 0.f) || wm >= (float)(1 << kMost) || !(f[0] + f[1] < __builtin_inff()))) {
       float y = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) y = fmaxf(y, p[j] * vs[j >> 2]);
@@ -306,10 +308,8 @@ __device__ __forceinline__ void decode_split_q8(const DecodeArgs& a, const float
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[d][i] = __builtin_ldexpf(o[d][i], to - k);
       k = to;
-      f[0] = __builtin_ldexpf(vs[0], k);
-      f[1] = __builtin_ldexpf(vs[1], k);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = p[j] * f[j >> 2];
+      for (int j = 0; j < 8; ++j) w[j] = __builtin_ldexpf(p[j] * vs[j >> 2], k);
     }
     f16x8_t ph;
 #pragma unroll

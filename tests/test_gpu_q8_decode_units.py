@@ -58,3 +58,23 @@ def test_large_values_then_higher_scores(fmt, b, g, ratio, splits):
     p = Pair(1, 2, L, b, fmt, [L])
     p.store(k, v, [0, L], [L])
     verify(p, q.cuda(), L, splits, f"{fmt} b={b} 2^{ratio}")
+
+
+@pytest.mark.parametrize("splits", [1, 2])
+@pytest.mark.parametrize("small", [0.0, 2.0 ** -90])
+@pytest.mark.parametrize("large", [2.0 ** 20, 2.0 ** 60, 2.0 ** 90])
+@pytest.mark.parametrize("fmt,b", [("int8", 16), ("e4m3", 64)])
+def test_values_of_zero_and_large_ones_without_weight(fmt, b, large, small, splits):
+    """Zeros (a scale of 2^-100 / Q) hold all the weight; the large values that
+    follow have a weight of zero, for one head exactly."""
+    L = 384 * splits
+    k, v = rows(L, 1, 1310)
+    v[:128 * splits] *= small
+    v[128 * splits:] *= large
+    k[:, 0, 0] = 0
+    k[128 * splits:, 0, 0] = -300.0
+    q = randn((1, 2, D), 1311)
+    q[0, 0, 0], q[0, 1, 0] = 40.0, 2.0
+    p = Pair(1, 1, L, b, fmt, [L])
+    p.store(k, v, [0, L], [L])
+    verify(p, q.cuda(), L, splits, f"{fmt} b={b} {small} {large}")
