@@ -487,20 +487,25 @@ class KVCacheQ8:
         return self._described()[1]
 
     def _described(self):
-        """(the cache's memory, its description, a reference to that, batch, kv
-        heads). The tensors are checked once, and again after one was replaced or
-        its memory moved (checking them took 8 us a call)."""
-        table = self.block_table
-        where = (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
-                 self.kmin.data_ptr(), self.kmax.data_ptr(), None if table is None else table.data_ptr())
+        """(what was checked, the cache's description, a reference to that, batch,
+        kv heads). The tensors are checked once, and again after one was replaced
+        or has another address, shape, type or order (checking them takes 8 us,
+        seeing that nothing has changed 1.5)."""
+        k, v, ks, vs, lo, hi, table = (self.k, self.v, self.k_scale, self.v_scale, self.kmin, self.kmax,
+                                       self.block_table)
+        seen = (k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), lo.data_ptr(), hi.data_ptr(), k.shape,
+                v.shape, ks.shape, vs.shape, lo.shape, hi.shape, k.dtype, v.dtype, ks.dtype, vs.dtype, lo.dtype,
+                hi.dtype, None if table is None else (table.data_ptr(), table.shape, table.dtype))
         checked = self._checked
-        if checked is not None and checked[0] == where:
+        if checked is not None and checked[0] == seen and k.is_contiguous() and v.is_contiguous() \
+                and ks.is_contiguous() and vs.is_contiguous() and lo.is_contiguous() and hi.is_contiguous() \
+                and (table is None or table.is_contiguous()):
             return checked
-        k, b = self.k, self.block_size
+        b = self.block_size
         fmt = _Q8_FORMATS.get(k.dtype)
         if fmt is None:
             raise TypeError(f"k must be torch.int8 or torch.float8_e4m3fn, got {k.dtype}")
-        B, H, mb = self.kmin.shape[:3]
+        B, H, mb = lo.shape[:3]
         if table is None:
             shape, pages, tp, scales = (B, H, mb * b, HEAD_DIM), 0, None, (B, H, mb)
         else:
@@ -508,15 +513,15 @@ class KVCacheQ8:
             shape, scales = (pages, H, b, HEAD_DIM), (pages, H)
             tp = _need(table, "block_table", torch.int32, (B, mb)).data_ptr()
         _need(k, "k", k.dtype, shape)
-        _need(self.v, "v", k.dtype, shape)
-        _need(self.k_scale, "k_scale", torch.float32, scales)
-        _need(self.v_scale, "v_scale", torch.float32, scales)
-        _need(self.kmin, "kmin", torch.bfloat16, (B, H, mb, HEAD_DIM))
-        _need(self.kmax, "kmax", torch.bfloat16, (B, H, mb, HEAD_DIM))
-        _one_device(k, self.v, self.k_scale, self.v_scale, self.kmin, self.kmax, table)
-        d = KVCacheQ8Desc(KVCacheDesc(where[0], where[1], where[4], where[5], B, H, HEAD_DIM, mb * b, b, tp, pages),
-                          where[2], where[3], fmt)
-        checked = (where, d, C.byref(d), B, H)
+        _need(v, "v", k.dtype, shape)
+        _need(ks, "k_scale", torch.float32, scales)
+        _need(vs, "v_scale", torch.float32, scales)
+        _need(lo, "kmin", torch.bfloat16, (B, H, mb, HEAD_DIM))
+        _need(hi, "kmax", torch.bfloat16, (B, H, mb, HEAD_DIM))
+        _one_device(k, v, ks, vs, lo, hi, table)
+        d = KVCacheQ8Desc(KVCacheDesc(seen[0], seen[1], seen[4], seen[5], B, H, HEAD_DIM, mb * b, b, tp, pages),
+                          seen[2], seen[3], fmt)
+        checked = (seen, d, C.byref(d), B, H)
         object.__setattr__(self, "_checked", checked)
         return checked
 

@@ -1,0 +1,74 @@
+"""The description that an 8-bit cache hands to the library, on CPU tensors that
+call themselves GPU tensors: no call here reaches the library's device code."""
+import pytest
+import torch
+
+import paper_2506_04108_amd as R
+
+B, H, CAP, BS, PAGES = 4, 2, 64, 16, 8
+
+
+class OnGpu(torch.Tensor):
+    is_cuda = True
+
+
+def on_gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+@pytest.fixture(params=[False, True], ids=["contiguous", "paged"])
+def cache(request, monkeypatch):
+    monkeypatch.setattr(R, "_devices", 1)
+    c = (R.KVCacheQ8.empty_paged(B, H, CAP, BS, PAGES, device="cpu") if request.param
+         else R.KVCacheQ8.empty(B, H, CAP, BS, device="cpu"))
+    for name in ("k", "v", "k_scale", "v_scale", "kmin", "kmax", "block_table"):
+        if getattr(c, name) is not None:
+            setattr(c, name, on_gpu(getattr(c, name)))
+    c.desc_q8()
+    return c
+
+
+def tensors(c):
+    return {n: getattr(c, n) for n in ("k", "v", "k_scale", "v_scale", "kmin", "kmax", "block_table")
+            if getattr(c, n) is not None}
+
+
+def test_fewer_sequences_or_pages_at_the_same_address(cache):
+    for name, t in tensors(cache).items():
+        t.set_(t[:2])
+    d = cache.desc_q8()
+    assert d.base.batch == 2 and d.base.num_pages == (2 if cache.paged else 0)
+    assert d.base.k == cache.k.data_ptr() and d.base.capacity == CAP
+
+
+def test_pool_of_fewer_pages(cache):
+    if not cache.paged:
+        pytest.skip("a pool")
+    for name in ("k", "v", "k_scale", "v_scale"):
+        t = getattr(cache, name)
+        t.set_(t[:4])
+    assert cache.desc_q8().base.num_pages == 4
+
+
+def test_codes_of_another_format_at_the_same_address(cache):
+    assert cache.desc_q8().format == 0
+    for t in (cache.k, cache.v):
+        t.data = t.data.view(torch.float8_e4m3fn)
+    assert cache.desc_q8().format == 1
+
+
+@pytest.mark.parametrize("name", ["k", "v", "k_scale", "v_scale", "kmin", "kmax", "block_table"])
+@pytest.mark.parametrize("change", ["rows", "strides", "type"])
+def test_one_tensor_that_no_longer_fits(cache, name, change):
+    t = getattr(cache, name)
+    if t is None:
+        pytest.skip("no table")
+    if change == "rows":
+        t.set_(t[:1])
+    elif change == "strides":
+        t.as_strided_(t.shape, (0,) * t.dim())
+    else:
+        t.data = t.data.view({1: torch.uint8, 2: torch.int16, 4: torch.int32}[t.element_size()]
+                             if name != "block_table" else torch.float32)
+    with pytest.raises((TypeError, ValueError)):
+        cache.desc_q8()
