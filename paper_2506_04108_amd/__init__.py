@@ -482,6 +482,10 @@ class KVCacheQ8:
         object.__setattr__(self, name, value)
         object.__setattr__(self, "_checked", None)
 
+    def __getstate__(self):
+        # A copy is checked by itself (and a description holds addresses).
+        return {**self.__dict__, "_checked": None}
+
     def desc_q8(self) -> KVCacheQ8Desc:
         """The library's description of this cache."""
         return self._described()[1]

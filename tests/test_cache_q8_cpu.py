@@ -1,5 +1,9 @@
 """The description that an 8-bit cache hands to the library, on CPU tensors that
 call themselves GPU tensors: no call here reaches the library's device code."""
+import copy
+import dataclasses
+import pickle
+
 import pytest
 import torch
 
@@ -72,3 +76,26 @@ def test_one_tensor_that_no_longer_fits(cache, name, change):
                              if name != "block_table" else torch.float32)
     with pytest.raises((TypeError, ValueError)):
         cache.desc_q8()
+
+
+@pytest.mark.parametrize("used", [False, True])
+def test_copies(used, monkeypatch):
+    """Copies and pickles of a cache, before its first call and after it."""
+    monkeypatch.setattr(R, "_devices", 1)
+    c = R.KVCacheQ8.empty_paged(B, H, CAP, BS, PAGES, device="cpu")
+    c.k.fill_(3)
+    if used:
+        gpu = R.KVCacheQ8(*(on_gpu(t) for t in (c.k, c.v, c.k_scale, c.v_scale, c.kmin, c.kmax)), BS,
+                          on_gpu(c.block_table))
+        gpu.desc_q8()
+        shallow = copy.copy(gpu)
+        assert shallow.k is gpu.k and shallow.desc_q8().base.k == gpu.k.data_ptr()
+        shallow.block_table = on_gpu(gpu.block_table.clone())
+        assert shallow.desc_q8().base.block_table != gpu.desc_q8().base.block_table
+        c._checked = gpu._checked
+    for d in (copy.deepcopy(c), pickle.loads(pickle.dumps(c)), dataclasses.replace(c)):
+        assert isinstance(d, R.KVCacheQ8) and d.block_size == BS and d.capacity == CAP and d.paged
+        for name, t in tensors(c).items():
+            assert torch.equal(getattr(d, name).view(torch.int8), t.view(torch.int8)), name
+        with pytest.raises(ValueError, match="on the GPU"):
+            d.desc_q8()
