@@ -92,7 +92,7 @@ def test_copies(used, monkeypatch):
         assert shallow.k is gpu.k and shallow.desc_q8().base.k == gpu.k.data_ptr()
         shallow.block_table = on_gpu(gpu.block_table.clone())
         assert shallow.desc_q8().base.block_table != gpu.desc_q8().base.block_table
-        c._checked = gpu._checked
+        object.__setattr__(c, "_checked", gpu._checked)
     for d in (copy.deepcopy(c), pickle.loads(pickle.dumps(c)), dataclasses.replace(c)):
         assert isinstance(d, R.KVCacheQ8) and d.block_size == BS and d.capacity == CAP and d.paged
         for name, t in tensors(c).items():
