@@ -30,6 +30,7 @@ import dataclasses
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 from ._lib import KVCacheDesc, KVCacheQ8Desc, ResaError, SelectParams, check, lib
 
@@ -530,13 +531,21 @@ class KVCacheQ8:
         return checked
 
 
+def _no_gradient(t: torch.Tensor, name: str) -> None:
+    """Refuses what a call would silently drop: a gradient asked for, or a tangent."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient: there is no backward pass")
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} has a tangent: there is no forward-mode derivative")
+
+
 def _packed(t: torch.Tensor, name: str, rows: int, heads: int) -> int:
     """Checks packed rows ``[rows, heads, 128]`` (bf16, a row contiguous) and
     returns the elements from one row to the next."""
     try:  # the usual case in one expression
         row, head, dim = t.stride()
         if t.dtype is torch.bfloat16 and t.is_cuda and t.shape == (rows, heads, HEAD_DIM) and dim == 1 \
-                and head == HEAD_DIM and not t.requires_grad:
+                and head == HEAD_DIM and not t.requires_grad and forward_ad._current_level < 0:
             return row if rows > 1 else heads * HEAD_DIM
     except (AttributeError, TypeError, ValueError):
         pass
@@ -548,8 +557,7 @@ def _packed(t: torch.Tensor, name: str, rows: int, heads: int) -> int:
         raise ValueError(f"{name} must be on the GPU")
     if t.shape != (rows, heads, HEAD_DIM):
         raise ValueError(f"{name} must have shape {(rows, heads, HEAD_DIM)}, got {tuple(t.shape)}")
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name} requires a gradient: there is no backward pass")
+    _no_gradient(t, name)
     row, head, dim = t.stride()
     if rows and (dim != 1 or (heads > 1 and head != HEAD_DIM)):
         raise ValueError(f"{name} must be contiguous within a row")
@@ -676,6 +684,7 @@ def sparse_decode_q8(cache: KVCacheQ8, q: torch.Tensor, seq_lens: torch.Tensor, 
     _, _, ref, B, H = cache._described()
     hq, n_cap = q.shape[1], block_idx.shape[-1]
     _need(q, "q", torch.bfloat16, (B, hq, HEAD_DIM))
+    _no_gradient(q, "q")
     _need(seq_lens, "seq_lens", torch.int32, (B,))
     _need(block_idx, "block_idx", torch.int32, (B, H, n_cap))
     _need(num_sel, "num_sel", torch.int32, (B, H))

@@ -99,3 +99,27 @@ def test_copies(used, monkeypatch):
             assert torch.equal(getattr(d, name).view(torch.int8), t.view(torch.int8)), name
         with pytest.raises(ValueError, match="on the GPU"):
             d.desc_q8()
+
+
+def calls(c):
+    """Each call that takes rows, as a function of one of its tensors, and that tensor."""
+    x, cu, lens = on_gpu(torch.zeros((3, H, 128), dtype=torch.bfloat16)), on_gpu(torch.zeros(B + 1, dtype=torch.int32)), \
+        on_gpu(torch.zeros(B, dtype=torch.int32))
+    q = on_gpu(torch.zeros((B, H, 128), dtype=torch.bfloat16))
+    idx, n = on_gpu(torch.zeros((B, H, 1), dtype=torch.int32)), on_gpu(torch.zeros((B, H), dtype=torch.int32))
+    return {
+        "prompt": (x, lambda t: R.prompt_attention(x, t, x, cu)),
+        "store": (x, lambda t: R.store_rows_q8(c, x, t, cu, lens)),
+        "decode": (q, lambda t: R.sparse_decode_q8(c, t, lens, idx, n)),
+        "rectify": (x, lambda t: R.dense_rectify_q8(c, t, x, x, cu, lens, CAP)),
+    }
+
+
+@pytest.mark.parametrize("name", ["prompt", "store", "decode", "rectify"])
+def test_gradients_are_refused(cache, name):
+    t, call = calls(cache)[name]
+    with pytest.raises(ValueError, match="requires a gradient"):
+        call(on_gpu(t.clone()).requires_grad_())
+    with torch.autograd.forward_ad.dual_level():
+        with pytest.raises(ValueError, match="tangent"):
+            call(torch.autograd.forward_ad.make_dual(t, on_gpu(torch.ones_like(t))))
