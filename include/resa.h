@@ -28,7 +28,10 @@
  * - Every tensor argument is a DEVICE pointer to caller-owned memory
  *   (usually allocated by PyTorch). The library never allocates, frees or
  *   synchronises; scratch comes from a caller workspace sized by the matching
- *   resa_*_workspace_size() call.
+ *   resa_*_workspace_size() call. What a workspace that has to be zero-filled
+ *   keeps between calls lies at places that follow from the batch and the kv
+ *   heads: one serves one operation at one batch and head count, and is
+ *   zero-filled again before another one uses it.
  * - Calls are asynchronous on the HIP stream passed as `stream` (a
  *   hipStream_t; NULL is the default stream). A call returns once its kernels
  *   are enqueued.

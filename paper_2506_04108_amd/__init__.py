@@ -176,15 +176,30 @@ class Workspace:
     Use one per operation kind. The decode kernel keeps one merge counter per
     group at the start of its workspace and leaves it at zero after every
     call (and a count of merged calls that tags its ready flags), so the
-    buffer is cleared only when it is (re)allocated. Calls that
-    share a workspace must be ordered on one stream.
+    buffer is cleared only when it is (re)allocated. Where what is kept lies
+    follows from the batch and the kv heads: each operation of each batch and
+    head count has a buffer of its own here, and ``buf`` is the one used last.
+    Calls that share a workspace must be ordered on one stream.
     """
 
     def __init__(self, device="cuda"):
         self.device = device
         self.buf = None
+        self._layout = None  # what buf is used as: (operation, batch, kv heads)
+        self._others = {}    # buffers of the other layouts
 
-    def get(self, nbytes: int) -> torch.Tensor:
+    def turn_to(self, layout: tuple) -> torch.Tensor | None:
+        """The buffer of a layout, if there is one (an unused one becomes it)."""
+        if layout != self._layout:
+            if self._layout is not None:
+                self._others[self._layout] = self.buf
+                self.buf = self._others.pop(layout, None)
+            self._layout = layout
+        return self.buf
+
+    def get(self, nbytes: int, layout: tuple | None = None) -> torch.Tensor:
+        if layout is not None:
+            self.turn_to(layout)
         if self.buf is None or self.buf.numel() < nbytes:
             self.buf = torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=self.device)
         return self.buf
@@ -250,7 +265,7 @@ def select_blocks(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, max_s
     if scores_out is not None:
         _need(scores_out, "scores_out", torch.float32, (B, Hkv, mseq))
     ws_bytes = lib().resa_select_workspace_size(B, Hkv, max_seq_len, cache.block_size)
-    ws = (workspace or Workspace(q.device)).get(ws_bytes)
+    ws = (workspace or Workspace(q.device)).get(ws_bytes, ("select", B, Hkv))
     ws_ptr, ws_bytes = ws.data_ptr(), ws.numel()
     params = SelectParams(float(sparsity), int(min_blocks), int(n_local))
     d = cache.desc_q8().base if isinstance(cache, KVCacheQ8) else cache.desc()
@@ -289,7 +304,7 @@ def append_select(cache: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, q: t
     if scores_out is not None:
         _need(scores_out, "scores_out", torch.float32, (B, Hkv, mseq))
     ws_bytes = lib().resa_select_workspace_size(B, Hkv, sel_len, cache.block_size)
-    ws = (workspace or Workspace(q.device)).get(ws_bytes)
+    ws = (workspace or Workspace(q.device)).get(ws_bytes, ("select", B, Hkv))
     params = SelectParams(float(sparsity), int(min_blocks), int(n_local))
     d = cache.desc()
     check(lib().resa_append_select(C.byref(d), k_new.data_ptr(), v_new.data_ptr(), q.data_ptr(), hq,
@@ -322,7 +337,7 @@ def sparse_decode(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, block
     if lse is not None:
         _need(lse, "lse", torch.float32, (B, hq))
     ws_bytes = lib().resa_decode_workspace_size(B, Hkv, hq, n_cap, cache.block_size, num_splits)
-    ws = (workspace or Workspace(q.device)).get(ws_bytes)
+    ws = (workspace or Workspace(q.device)).get(ws_bytes, ("decode", B, Hkv))
     d = cache.desc()
     check(lib().resa_sparse_decode(C.byref(d), q.data_ptr(), hq, seq_lens.data_ptr(),
                                    block_idx.data_ptr(), num_sel.data_ptr(), n_cap, num_splits,
@@ -370,7 +385,7 @@ def decode_step(cache: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, q: tor
         _need(lse, "lse", torch.float32, (B, hq))
     ws_bytes = lib().resa_step_workspace_size(B, Hkv, hq, max_seq_len, cache.block_size, n_cap,
                                               num_splits)
-    ws = (workspace or Workspace(q.device)).get(ws_bytes)
+    ws = (workspace or Workspace(q.device)).get(ws_bytes, ("step", B, Hkv))
     params = SelectParams(float(sparsity), int(min_blocks), int(n_local))
     d = cache.desc()
     check(lib().resa_decode_step(C.byref(d), k_new.data_ptr(), v_new.data_ptr(), q.data_ptr(), hq,
@@ -407,7 +422,7 @@ def dense_rectify(cache: KVCache, q_f: torch.Tensor, k_f: torch.Tensor, v_f: tor
     if lse is not None:
         _need(lse, "lse", torch.float32, (B, hq, f))
     ws_bytes = lib().resa_rectify_workspace_size(B, Hkv, hq, f, max_seq_len)
-    ws = (workspace or Workspace(q_f.device)).get(ws_bytes)
+    ws = (workspace or Workspace(q_f.device)).get(ws_bytes, ("rectify",))
     d = cache.desc()
     check(lib().resa_dense_rectify(C.byref(d), q_f.data_ptr(), k_f.data_ptr(), v_f.data_ptr(), hq, f,
                                    seq_lens.data_ptr(), _ptr(seq_mask), max_seq_len, float(sm_scale),
@@ -589,16 +604,17 @@ def _new(stream, like: torch.Tensor, *wanted):
         return [like.new_empty(shape, dtype=dtype, requires_grad=False) for shape, dtype in wanted]
 
 
-def _with_workspace(call, needs, workspace, stream, device):
-    """call(pointer, bytes) on the workspace as it is; where the library finds it
-    too small (before it enqueues anything), on one of needs() bytes."""
-    ws = workspace.buf if workspace is not None else None
+def _with_workspace(call, needs, workspace, layout, stream, device):
+    """call(pointer, bytes) on the workspace's buffer of that layout as it is; where
+    the library finds it too small (before it enqueues anything), on one of
+    needs() bytes."""
+    ws = workspace.turn_to(layout) if workspace is not None else None
     if ws is not None:
         rc = call(ws.data_ptr(), ws.numel())
         if rc != _ERR_WORKSPACE:
             return check(rc)
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-        ws = (workspace or Workspace(device)).get(needs())
+        ws = (workspace or Workspace(device)).get(needs(), layout)
     check(call(ws.data_ptr(), ws.numel()))
 
 
@@ -702,7 +718,7 @@ def sparse_decode_q8(cache: KVCacheQ8, q: torch.Tensor, seq_lens: torch.Tensor, 
     run, st = lib().resa_sparse_decode_q8, _stream(stream)
     _with_workspace(lambda ws, size: run(*ptrs, ws, size, st),
                     lambda: lib().resa_decode_q8_workspace_size(B, H, hq, n_cap, cache.block_size, num_splits),
-                    workspace, stream, q.device)
+                    workspace, ("decode", B, H), stream, q.device)
     return out, lse
 
 
@@ -738,5 +754,5 @@ def dense_rectify_q8(cache: KVCacheQ8, q_rows: torch.Tensor, k_rows: torch.Tenso
         run, st = lib().resa_dense_rectify_q8, _stream(stream)
         _with_workspace(lambda ws, size: run(*ptrs, ws, size, st),
                         lambda: lib().resa_rectify_q8_workspace_size(B, H, hq, T, max_seq_len),
-                        workspace, stream, q_rows.device)
+                        workspace, ("rectify",), stream, q_rows.device)
     return out, lse
