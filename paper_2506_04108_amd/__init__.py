@@ -179,7 +179,8 @@ class Workspace:
     buffer is cleared only when it is (re)allocated. Where what is kept lies
     follows from the batch and the kv heads: each operation of each batch and
     head count has a buffer of its own here, and ``buf`` is the one used last.
-    Calls that share a workspace must be ordered on one stream.
+    A buffer that a call recorded in a graph uses stays as it is when a later
+    call needs a larger one. Calls that share a workspace must be ordered on one stream.
     """
 
     def __init__(self, device="cuda"):
@@ -187,6 +188,7 @@ class Workspace:
         self.buf = None
         self._layout = None  # what buf is used as: (operation, batch, kv heads)
         self._others = {}    # buffers of the other layouts
+        self._recorded = []  # buffers that recorded calls use
 
     def turn_to(self, layout: tuple) -> torch.Tensor | None:
         """The buffer of a layout, if there is one (an unused one becomes it)."""
@@ -197,11 +199,18 @@ class Workspace:
             self._layout = layout
         return self.buf
 
+    def record(self) -> None:
+        """Keeps the buffer at hand where the call that uses it is being recorded."""
+        if self.buf.is_cuda and torch.cuda.is_current_stream_capturing() \
+                and not any(b is self.buf for b in self._recorded):
+            self._recorded.append(self.buf)
+
     def get(self, nbytes: int, layout: tuple | None = None) -> torch.Tensor:
         if layout is not None:
             self.turn_to(layout)
         if self.buf is None or self.buf.numel() < nbytes:
             self.buf = torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        self.record()
         return self.buf
 
 
@@ -612,6 +621,7 @@ def _with_workspace(call, needs, workspace, layout, stream, device):
     if ws is not None:
         rc = call(ws.data_ptr(), ws.numel())
         if rc != _ERR_WORKSPACE:
+            workspace.record()
             return check(rc)
     with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
         ws = (workspace or Workspace(device)).get(needs(), layout)

@@ -84,3 +84,29 @@ def test_graphs_in_turn():
                 assert torch.equal(x, y), i
             for x, y in zip(eager, want[(i + 1) % 6]):
                 assert torch.equal(x, y), (i, "eager")
+
+
+@pytest.mark.parametrize("kind", ["decode", "rectify"])
+def test_graph_before_a_larger_call(kind):
+    """A graph recorded on a small buffer, replayed after a larger call took a
+    larger one and other tensors came and went."""
+    ws = R.Workspace()
+    small, large = ((decode_call(2, 2, 700, 21, 4), decode_call(2, 2, 900, 22, 200)) if kind == "decode" else
+                    (rectify_call(1, 2, 1500, 2, 23), rectify_call(1, 2, 9000, 16, 24)))
+    want, want_large = ([x.clone() for x in c()] for c in (small, large))
+    out, lse = small(workspace=ws)
+    torch.cuda.synchronize()
+    graph, size = torch.cuda.CUDAGraph(), ws.buf.numel()
+    with torch.cuda.graph(graph):
+        small(out=out, lse=lse, workspace=ws)
+    for turn in range(3):
+        got = large(workspace=ws)
+        assert ws.buf.numel() > size
+        junk = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        out.fill_(float("nan")), lse.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all((j == 255).all() for j in junk), turn
+        for x, y in zip((out, lse, *got), (*want, *want_large)):
+            assert torch.equal(x, y), turn
+        del junk

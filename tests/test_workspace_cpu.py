@@ -1,4 +1,7 @@
 """What a Workspace hands out, on the CPU."""
+import gc
+import weakref
+
 import torch
 
 import paper_2506_04108_amd as R
@@ -28,3 +31,25 @@ def test_a_buffer_sized_beforehand():
     a = ws.get(4096)
     assert ws.get(100, ("step", 1, 2)) is a and ws.get(50) is a
     assert ws.get(100, ("step", 2, 2)) is not a
+
+
+def test_a_recorded_buffer_stays(monkeypatch):
+    """A larger buffer does not free the one whose address a graph holds."""
+    class OnGpu(torch.Tensor):
+        is_cuda = True
+
+    zeros = torch.zeros
+    monkeypatch.setattr(torch, "zeros", lambda *size, **kw: zeros(*size, **kw).as_subclass(OnGpu))
+    ws, recording = R.Workspace("cpu"), [True]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: recording[0])
+    first = weakref.ref(ws.get(1000, ("decode", 1, 1)))
+    second = weakref.ref(ws.get(2000, ("decode", 1, 1)))
+    recording[0] = False
+    third = weakref.ref(ws.get(3000, ("decode", 1, 1)))
+    ws.get(4000, ("decode", 1, 1))
+    gc.collect()
+    assert first() is not None and second() is not None and third() is None
+    recording[0] = True
+    for _ in range(3):
+        ws.get(100)
+    assert len(ws._recorded) == 3
