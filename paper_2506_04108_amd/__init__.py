@@ -27,6 +27,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import dataclasses
+import functools
 import math
 
 import torch
@@ -61,6 +62,19 @@ def _current_raw_stream(device: int) -> int:
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_raw_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _on_its_stream(call):
+    """A call given a stream makes its new tensors there too: a workspace is
+    cleared in order with the kernels, and no memory goes back to another
+    stream while they run."""
+    @functools.wraps(call)
+    def wrapper(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            return call(*args, **kw)
+    return wrapper
 
 
 def _need(t: torch.Tensor, name: str, dtype, shape=None):
@@ -247,6 +261,7 @@ def append_kv(cache: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, seq_lens
                                max_seq_len, _stream(stream)))
 
 
+@_on_its_stream
 def select_blocks(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, max_seq_len: int,
                   sparsity: float, min_blocks: int, n_local: int = 1, n_cap: int | None = None,
                   block_idx: torch.Tensor | None = None, num_sel: torch.Tensor | None = None,
@@ -284,6 +299,7 @@ def select_blocks(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, max_s
     return block_idx, num_sel
 
 
+@_on_its_stream
 def append_select(cache: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, q: torch.Tensor,
                   seq_lens: torch.Tensor, max_seq_len: int, sparsity: float, min_blocks: int,
                   n_local: int = 1, n_cap: int | None = None, block_idx: torch.Tensor | None = None,
@@ -323,6 +339,7 @@ def append_select(cache: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, q: t
     return block_idx, num_sel
 
 
+@_on_its_stream
 def sparse_decode(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, block_idx: torch.Tensor,
                   num_sel: torch.Tensor, num_splits: int = 0, sm_scale: float | None = None,
                   out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
@@ -355,6 +372,7 @@ def sparse_decode(cache: KVCache, q: torch.Tensor, seq_lens: torch.Tensor, block
     return out, lse
 
 
+@_on_its_stream
 def decode_step(cache: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, q: torch.Tensor,
                 seq_lens: torch.Tensor, max_seq_len: int, sparsity: float, min_blocks: int,
                 n_local: int = 1, n_cap: int | None = None, num_splits: int = 0,
@@ -405,6 +423,7 @@ def decode_step(cache: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, q: tor
     return block_idx, num_sel, out, lse
 
 
+@_on_its_stream
 def dense_rectify(cache: KVCache, q_f: torch.Tensor, k_f: torch.Tensor, v_f: torch.Tensor,
                   seq_lens: torch.Tensor, max_seq_len: int, sm_scale: float | None = None,
                   out: torch.Tensor | None = None, lse: torch.Tensor | None = None,

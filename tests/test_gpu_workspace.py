@@ -110,3 +110,24 @@ def test_graph_before_a_larger_call(kind):
         for x, y in zip((out, lse, *got), (*want, *want_large)):
             assert torch.equal(x, y), turn
         del junk
+
+
+@pytest.mark.parametrize("i", range(5))
+def test_calls_on_a_stream_while_the_current_one_is_busy(i):
+    """Nothing of a call on a side stream waits for the current stream, or
+    overtakes what it needs there."""
+    call = some_calls()[i]
+    want = [x.clone() for x in call()]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        junk = [torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        del junk
+        torch.cuda._sleep(20_000_000)  # some 10 ms
+        got = call(stream=side)
+        side.synchronize()
+        with torch.cuda.stream(side):
+            same = [torch.equal(x, y) for x, y in zip(got, want)]
+        assert all(same)
+        torch.cuda.synchronize()
