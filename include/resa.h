@@ -398,7 +398,8 @@ int resa_dense_rectify(const resa_kv_cache_t* c, const void* q_f, const void* k_
  * the second product, out rounded to bf16; finite for |v| <= 2^96. What a token
  * does not see never reaches its row, infinities and NaN included.
  * Errors: RESA_ERR_INVALID_ARG (null or misaligned pointer, a size or stride
- * out of range, sm_scale not finite), RESA_ERR_UNSUPPORTED (head_dim, group).
+ * out of range, sm_scale not finite), RESA_ERR_UNSUPPORTED (head_dim, group,
+ * batch * num_kv_heads above 65535, more rows than a launch takes).
  */
 int resa_prompt_attention(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride,
                           int64_t v_stride, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
@@ -472,8 +473,9 @@ size_t resa_decode_q8_workspace_size(int32_t batch, int32_t num_kv_heads, int32_
 /*
  * resa_sparse_decode over an 8-bit cache: the same arguments, results (fp32 out
  * and lse) and workspace rules, for k = code * k_scale and v = code * v_scale.
- * Products of codes are exact, weights, sums and scales fp32. Codes of rows
- * past L_b and of blocks that are not selected are not used, whatever they
+ * Products of codes are exact, scales and sums fp32; a weight times the value
+ * scale of its block is the sum of two fp16 terms, 22 bits, down to 2^-36 of the
+ * largest that its head has met. Codes of rows past L_b and of blocks that are not selected are not used, whatever they
  * hold. A block whose scale is not finite makes the out of the query heads
  * that attend to it NaN. Value range as in resa_sparse_decode.
  */

@@ -37,9 +37,10 @@
 //
 // Bound by HBM (256 B a token and kv head) and, with few chunks a wave, by the
 // latency of a launch, the ids, the first codes and the merge. 64K batch 8 (108
-// MB), 256K batch 1 (27 MB), 50K batch 6 paged (40 MB), 4K batch 1: 25.1, 13.7,
-// 17.6, 8.9 us (HBM at a large copy's rate: 21, 5.3, 7.8, 0.4; with codes
-// through registers, the loads in the MFMAs' layouts: 29.3, 15.6, 23.4, 9.0).
+// MB), 256K batch 1 (27 MB), 50K batch 6 paged (40 MB), 4K batch 1: 24.4, 13.3,
+// 17.1, 8.5 us (HBM at a large copy's rate: 21, 5.3, 7.8, 0.4, at a large read's: 15,
+// 3.8, 5.6, 0.3; with codes through registers, the loads in the MFMAs' layouts:
+// 29.3, 15.6, 23.4, 9.0).
 // More chunks on their way are slower (two: 26.0, 13.8, 18.0 us, three: 27.5, 15.5,
 // 24.6), as in the bf16 decode, and so are 8 waves (25.6, 14.5, 16.9 us, 4K
 // 10.0). Both products on int8 digits, with no code converted and half of the

@@ -42,17 +42,17 @@
 // a round later through registers, converted under P.V's MFMAs, into the tiles.
 // 8 x 64K, 32 rows of 4 heads each: 402 -> 370 us a call against codes and
 // scales held in registers on their way (whose copies from one register to
-// another waited for the loads), at 2.0 GHz: the chip is at its power limit
-// here too, as in long prompts (1.75 GHz, the matrix cores busy 64 % of the
-// cycles and the VALU 55 %).
+// another waited for the loads). There the matrix cores are busy 40 % of the
+// cycles, the VALU 55 % and the LDS 61 %, at 1.9 GHz; the conversion costs less than
+// that suggests: int8, 6 instructions for four codes, 367 us, e4m3, 2, 351. One long
+// prompt: matrix cores 61 %, VALU 51 %, LDS 46 %, at 1.8 GHz of 2.4.
 //
-// Measured: one prompt of 16384 tokens, 32 heads over 8: 1.85 - 1.88 ms, 1.17 - 1.19
-// PFLOP/s; 16 prompts of 77 to 2000 tokens, 28 heads over 4: 207 - 219 us, 0.76 -
-// 0.81 PFLOP/s, the starts and ends of workgroups (block, queries, first tiles;
-// output: 10 us each) not all hidden by their neighbours; one of 300 tokens 10.1 us, a
-// chain of latencies. 32 rows of 4 heads behind 8 x 64K codes: 357 - 374 us with
-// the stores and the merge, 2.9 - 3.0 TB/s; 2033 rows of 7 behind 31K: 1.39 - 1.41
-// ms, 0.98 - 1.0 PFLOP/s.
+// Measured: one prompt of 16384 tokens, 32 heads over 8: 1.88 - 1.90 ms, 1.16 - 1.17
+// PFLOP/s; 16 prompts of 77 to 2000 tokens, 28 heads over 4: 211 us called again and
+// again, 226 with other inputs each time, 0.74 - 0.79 PFLOP/s; one of 300 tokens 10.0
+// us, a chain of latencies. 32 rows of 4 heads behind 8 x 64K codes: 364 - 369 us with
+// the stores and the merge, 2.9 - 3.0 TB/s; 2033 rows of 7 behind 31K: 1.41 ms, 0.98
+// PFLOP/s (int8 1.45).
 //
 // Masked keys: scores are replaced, so nothing of a masked K row matters; a
 // masked V row meets weights of zero, which only a value that is not finite

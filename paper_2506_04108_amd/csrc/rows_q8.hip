@@ -13,7 +13,9 @@
 // token: one wave per block, K and V in neighbouring waves, costs it one
 // round trip for the lengths and one for the rows. 8 prompts of up to 8180 rows,
 // 8 kv heads: 53 us to store (236 MB, 4.4 TB/s), 35 us to load (227 MB, 6.4 TB/s);
-// one token of 8 sequences 4.6 and 3.1 us.
+// one token of 8 sequences 4.6 and 3.1 us. The same prompts stored, or loaded, again
+// and again: 43 - 50 and 34 - 40 us in both formats, contiguous or paged, by blocks of
+// 16, 32 and 64.
 #include "rows_device.h"
 
 namespace resa {
