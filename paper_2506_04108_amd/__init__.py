@@ -190,33 +190,46 @@ class Workspace:
     Use one per operation kind. The decode kernel keeps one merge counter per
     group at the start of its workspace and leaves it at zero after every
     call (and a count of merged calls that tags its ready flags), so the
-    buffer is cleared only when it is (re)allocated. Where what is kept lies
-    follows from the batch and the kv heads: each operation of each batch and
-    head count has a buffer of its own here, and ``buf`` is the one used last.
-    A buffer that a call recorded in a graph uses stays as it is when a later
-    call needs a larger one. Calls that share a workspace must be ordered on one stream.
+    buffer is cleared only when it is (re)allocated, or when a call of another
+    operation, batch or head count takes it over: where what is kept lies
+    follows from these. A buffer that a call recorded in a graph uses is neither
+    taken over nor freed; ``buf`` is the one used last. Calls that share a
+    workspace must be ordered on one stream.
     """
 
     def __init__(self, device="cuda"):
         self.device = device
         self.buf = None
         self._layout = None  # what buf is used as: (operation, batch, kv heads)
-        self._others = {}    # buffers of the other layouts
         self._recorded = []  # buffers that recorded calls use
+        self._others = {}    # those of them that are used as something else than buf
+        self._spare = None   # a buffer that is not, while buf is one of them
+
+    def _is_recorded(self) -> bool:
+        return any(b is self.buf for b in self._recorded)
+
+    def _capturing(self) -> bool:
+        return self.buf.is_cuda and torch.cuda.is_current_stream_capturing()
 
     def turn_to(self, layout: tuple) -> torch.Tensor | None:
-        """The buffer of a layout, if there is one (an unused one becomes it)."""
+        """A buffer for calls of that layout, if there is one."""
         if layout != self._layout:
-            if self._layout is not None:
-                self._others[self._layout] = self.buf
-                self.buf = self._others.pop(layout, None)
+            unused = self._layout is None
+            if not unused and self.buf is not None and self._is_recorded():
+                self._others[self._layout], self.buf, self._spare = self.buf, self._spare, None
             self._layout = layout
+            if layout in self._others:
+                self._spare, self.buf = self.buf, self._others.pop(layout)
+            elif not unused and self.buf is not None:
+                if self._capturing():  # a graph is not to clear it each time
+                    self.buf = None
+                else:
+                    self.buf.zero_()
         return self.buf
 
     def record(self) -> None:
         """Keeps the buffer at hand where the call that uses it is being recorded."""
-        if self.buf.is_cuda and torch.cuda.is_current_stream_capturing() \
-                and not any(b is self.buf for b in self._recorded):
+        if self._capturing() and not self._is_recorded():
             self._recorded.append(self.buf)
 
     def get(self, nbytes: int, layout: tuple | None = None) -> torch.Tensor:
@@ -632,7 +645,7 @@ def _new(stream, like: torch.Tensor, *wanted):
         return [like.new_empty(shape, dtype=dtype, requires_grad=False) for shape, dtype in wanted]
 
 
-def _with_workspace(call, needs, workspace, layout, stream, device):
+def _with_workspace(call, needs, workspace, layout, device):
     """call(pointer, bytes) on the workspace's buffer of that layout as it is; where
     the library finds it too small (before it enqueues anything), on one of
     needs() bytes."""
@@ -642,8 +655,7 @@ def _with_workspace(call, needs, workspace, layout, stream, device):
         if rc != _ERR_WORKSPACE:
             workspace.record()
             return check(rc)
-    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-        ws = (workspace or Workspace(device)).get(needs(), layout)
+    ws = (workspace or Workspace(device)).get(needs(), layout)
     check(call(ws.data_ptr(), ws.numel()))
 
 
@@ -720,6 +732,7 @@ def load_rows_q8(cache: KVCacheQ8, cu_rows: torch.Tensor, seq_lens: torch.Tensor
     return k_rows, v_rows
 
 
+@_on_its_stream
 def sparse_decode_q8(cache: KVCacheQ8, q: torch.Tensor, seq_lens: torch.Tensor, block_idx: torch.Tensor,
                      num_sel: torch.Tensor, num_splits: int = 0, sm_scale: float | None = None,
                      out: torch.Tensor | None = None, lse: torch.Tensor | None = None, with_lse: bool = True,
@@ -747,10 +760,11 @@ def sparse_decode_q8(cache: KVCacheQ8, q: torch.Tensor, seq_lens: torch.Tensor, 
     run, st = lib().resa_sparse_decode_q8, _stream(stream)
     _with_workspace(lambda ws, size: run(*ptrs, ws, size, st),
                     lambda: lib().resa_decode_q8_workspace_size(B, H, hq, n_cap, cache.block_size, num_splits),
-                    workspace, ("decode", B, H), stream, q.device)
+                    workspace, ("decode", B, H), q.device)
     return out, lse
 
 
+@_on_its_stream
 def dense_rectify_q8(cache: KVCacheQ8, q_rows: torch.Tensor, k_rows: torch.Tensor, v_rows: torch.Tensor,
                      cu_rows: torch.Tensor, seq_lens: torch.Tensor, max_seq_len: int,
                      sm_scale: float | None = None, out: torch.Tensor | None = None,
@@ -783,5 +797,5 @@ def dense_rectify_q8(cache: KVCacheQ8, q_rows: torch.Tensor, k_rows: torch.Tenso
         run, st = lib().resa_dense_rectify_q8, _stream(stream)
         _with_workspace(lambda ws, size: run(*ptrs, ws, size, st),
                         lambda: lib().resa_rectify_q8_workspace_size(B, H, hq, T, max_seq_len),
-                        workspace, ("rectify",), stream, q_rows.device)
+                        workspace, ("rectify",), q_rows.device)
     return out, lse
