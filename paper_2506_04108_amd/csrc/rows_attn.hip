@@ -49,9 +49,9 @@
 //
 // Measured: one prompt of 16384 tokens, 32 heads over 8: 1.88 - 1.90 ms, 1.16 - 1.17
 // PFLOP/s; 16 prompts of 77 to 2000 tokens, 28 heads over 4: 211 us called again and
-// again, 226 with other inputs each time, 0.74 - 0.79 PFLOP/s; one of 300 tokens 10.0
-// us, a chain of latencies. 32 rows of 4 heads behind 8 x 64K codes: 364 - 369 us with
-// the stores and the merge, 2.9 - 3.0 TB/s; 2033 rows of 7 behind 31K: 1.41 ms, 0.98
+// again, 226 - 231 with other inputs each time, 0.72 - 0.79 PFLOP/s; one of 300 tokens 10.0
+// us, a chain of latencies. 32 rows of 4 heads behind 8 x 64K codes: 364 - 372 us with
+// the stores and the merge, 2.9 - 3.0 TB/s; 2033 rows of 7 behind 31K: 1.41 - 1.43 ms, 0.98
 // PFLOP/s (int8 1.45).
 //
 // Masked keys: scores are replaced, so nothing of a masked K row matters; a
